@@ -228,7 +228,8 @@ def prepare(case, seed):
         if case["direction"] == "gradient":
             state["dlogp"] = torch.randn((T,), generator=g, device="cuda") / T
             # what the forward call returned beside the log probabilities: the
-            # maximum and the logarithm of the sum, of logits over temperature
+            # largest logit, and the logarithm of the sum of the exponentials of
+            # the logits' distances from it over the temperature
             state["stats"] = _stats64(x, y, case["temperature"]).float()
         return state
     off = state["offsets"] = _offsets(case)
@@ -262,7 +263,7 @@ def _stats64(x, y, temperature):
     for r in range(0, x.shape[0], 1024):
         z = x[r:r + 1024].double() / temperature
         top = z.max(1).values
-        s = torch.stack([top, torch.log(torch.exp(z - top[:, None]).sum(1))], 1)
+        s = torch.stack([x[r:r + 1024].amax(1).double(), torch.log(torch.exp(z - top[:, None]).sum(1))], 1)
         out[r:r + 1024] = torch.where((y[r:r + 1024] >= 0)[:, None], s, torch.zeros_like(s))
     return out
 
@@ -337,10 +338,9 @@ def _plain_logprob(s, case):
         log_sum = torch.log(total)
         valid = y >= 0
         logp = torch.where(valid, _at_target(z, y) - top - log_sum, 0.0)
-        stats = torch.where(valid[:, None], torch.stack([top, log_sum], 1), 0.0)
+        stats = torch.where(valid[:, None], torch.stack([x.amax(1).float(), log_sum], 1), 0.0)
         return {"logp": logp, "stats": stats}
-    z = x.float() / tau
-    p = torch.exp(z - s["stats"][:, :1] - s["stats"][:, 1:])
+    p = torch.exp((x.float() - s["stats"][:, :1]) / tau - s["stats"][:, 1:])
     return {"dlogits": _row_gradient(p, y, s["dlogp"], tau, x.dtype)}
 
 
