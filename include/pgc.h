@@ -35,7 +35,7 @@ extern "C" {
 #define PGC_ENOTSUP  (-6)  /* valid but unsupported combination             */
 #define PGC_ETIMEOUT (-7)  /* a bounded device-side wait gave up            */
 #define PGC_ESCRATCH (-8)  /* problem larger than pgc_gradient_noalloc's
-                              fixed scratch                                 */
+                              fixed scratch, or than the workspace given    */
 #define PGC_ESINGULAR (-9) /* GC-CR: the draws leave a worker's encoding
                               system singular, or the encoding cannot decode
                               the straggler set                             */
@@ -380,6 +380,142 @@ int pgc_timing_read(pgc_ctx *ctx, double *ms, int64_t *launches, int64_t *steps_
  */
 int pgc_gradient_noalloc(int32_t loss, int32_t dtype, int64_t m, int64_t d, const void *X,
                          const float *y, const float *w, float *g_out, void *stream);
+
+/* ---- losses on rows of logits, with their gradients ------------------------ */
+
+/*
+ * The calls below take a caller's logits where a run's softmax loss forms its
+ * own: rows of V logits in device memory, one row per token, and give a loss
+ * and its gradient with respect to every logit.  The paper has no counterpart;
+ * they serve models whose last product is made elsewhere.
+ *
+ * With the temperature tau, the row's largest logit m and
+ * L = log sum_v exp((x_v - m) / tau), the target y of a row has
+ *   logp = (x_y - m) / tau - L,   d logp / d x_v = ([v = y] - p_v) / tau,
+ *   p_v = exp((x_v - m) / tau - L).
+ *
+ * Common to all of them:
+ *  - They keep no state and allocate nothing.  All pointers but the structure
+ *    itself are device pointers on the current device; the work is ordered on
+ *    `stream` (cudaStream_t; NULL = legacy stream) and the call returns without
+ *    waiting, so it can be captured into a CUDA graph.  Calls that may overlap
+ *    (two streams, two graphs) need workspaces and outputs of their own.
+ *  - workspace: 16-byte aligned device memory of the bytes that
+ *    pgc_loss_workspace / pgc_balance_workspace return; its contents do not
+ *    matter before a call and mean nothing after it.
+ *  - Sums, maxima and probabilities are held in 32 bits (sums over tokens in 64), a bf16
+ *    gradient is rounded once.  A call repeated on the same inputs gives the same bits.
+ *  - A row whose target is negative takes no part (prompts, padding): its logits are
+ *    not read, its log probability is 0 and its gradient row is zeros.  A
+ *    target >= classes is not followed: log probability, gradient row and
+ *    loss are NaN.  A row all of whose logits are -inf has no distribution: NaN
+ *    as well.  A target of logit -inf has log probability -inf.
+ *  - offsets: int32, sequence i is rows offsets[i] .. offsets[i + 1] - 1 (so
+ *    a padded batch is offsets of equal steps, its padding rows of negative
+ *    target).  Rows of no sequence take no part.  Offsets that fall or leave [0, rows]
+ *    are not followed: loss and gradients are NaN.  A sequence may be empty.
+ *  - Errors: PGC_EINVAL before any CUDA call (sizes, enumerations, NULL, alignment: logits
+ *    and gradient to their element, the rest to 4 bytes), PGC_ESCRATCH (workspace too small),
+ *    PGC_ENOTSUP where listed, PGC_ECUDA.
+ */
+typedef struct pgc_logits {
+  const void    *x;           /* logits: row t at x + t * ld elements              */
+  const int32_t *target;      /* [rows] class of each row, negative: none           */
+  void          *grad;        /* gradient, of the logits' type, row t at grad + t * grad_ld;
+                                 NULL: only the loss.  May be x itself (with
+                                 grad_ld = ld), otherwise it overlaps nothing       */
+  int64_t rows, classes;      /* 0 <= rows < 2^31, 1 <= classes < 2^31              */
+  int64_t ld, grad_ld;        /* row pitches in elements, classes <= ld <= 2^31     */
+  int32_t dtype;              /* PGC_F32 or PGC_BF16                                */
+  float   temperature;        /* tau > 0 (1: the logits as they are)                */
+} pgc_logits;
+
+/* pgc_loss_workspace — bytes of workspace of a preference or policy loss over
+ * `rows` rows and `sequences` sequences (two per pair; 0 without offsets).
+ * Errors: PGC_EINVAL. */
+int pgc_loss_workspace(int64_t rows, int64_t sequences, int64_t *bytes);
+
+/*
+ * pgc_token_logprob — logp[rows] = log probability of each row's target, and
+ * stats[rows][2] (8-byte aligned) = (m, L) of the row, for the gradient call; (0, 0)
+ * for a row without a target.  z->grad is not used.
+ */
+int pgc_token_logprob(const pgc_logits *z, float *logp, float *stats, void *stream);
+
+/*
+ * pgc_token_logprob_grad — z->grad[t][v] = dlogp[t] ([v = y_t] - p_tv) / tau:
+ * the gradient of any loss whose derivative with respect to the rows' log
+ * probabilities is dlogp[rows].  stats: as pgc_token_logprob returned them for the
+ * same logits.  A row whose dlogp is 0 gets zeros.
+ */
+int pgc_token_logprob_grad(const pgc_logits *z, const float *stats, const float *dlogp, void *stream);
+
+#define PGC_PREF_SIGMOID 0   /* (1-e) log(1 + exp(-h)) + e log(1 + exp(h))            */
+#define PGC_PREF_HINGE   1   /* (1-e) max(0, 1 - h) + e max(0, 1 + h)                 */
+#define PGC_PREF_SQUARED 2   /* (1-e) (h/beta - 1/(2 beta))^2 + e (h/beta + 1/(2 beta))^2 */
+
+/*
+ * pgc_preference_loss — paired log ratios.  Sequence 2 i is the chosen and
+ * 2 i + 1 the rejected answer of pair i; the score s of a sequence is the sum of
+ * its rows' log probabilities (average != 0: their mean; 0 for a sequence
+ * without targets), and
+ *   h_i = beta ((s_2i - r_2i) - (s_2i+1 - r_2i+1)) - margin
+ * with the reference scores r.  loss = scale / pairs * sum_i f(h_i), f by `kind`
+ * with e = smoothing (0 <= e <= 1).
+ *   offsets  : [2 pairs + 1].   ref_logp: [pairs][2], or NULL for zeros.
+ *   beta > 0, margin, scale finite.
+ *   loss     : [1];  logp: [pairs][2] receives the scores s.
+ * No pairs: the loss is 0.
+ */
+int pgc_preference_loss(const pgc_logits *z, int32_t kind, int64_t pairs, const int32_t *offsets, const float *ref_logp,
+                        float beta, float margin, float smoothing, int32_t average, float scale, float *loss,
+                        float *logp, void *workspace, int64_t workspace_bytes, void *stream);
+
+#define PGC_MEAN_TOKENS    0   /* every row with a target weighs 1 / their number      */
+#define PGC_MEAN_SEQUENCES 1   /* 1 / (its sequence's rows with a target x sequences that have one) */
+#define PGC_SUM            2   /* 1                                                    */
+
+/*
+ * pgc_policy_loss — clipped policy loss with a KL term.  For each row with a
+ * target, r = exp(logp - old_logp), A its advantage, q = r clamped to
+ * [1 - clip_low, 1 + clip_high], u = ref_logp - logp:
+ *   loss = scale * sum_t w_t (-min(r A, q A) + kl (exp(u) - u - 1)).
+ * The derivative is that of r A where r A <= q A, and 0 of q A elsewhere.
+ *   reduction: w_t, PGC_MEAN_* or PGC_SUM; offsets [sequences + 1] are read for
+ *     PGC_MEAN_SEQUENCES only.
+ *   old_logp, advantage: [rows].  ref_logp: [rows], or NULL (then kl must be 0).
+ *   0 <= clip_low <= 1, clip_high >= 0; kl, scale finite.
+ *   loss [1]; terms [3] = the weighted sums (without scale) of -min(r A, q A), of
+ *     exp(u) - u - 1 (0 without ref_logp) and of the rows where q A < r A.
+ *   logp [rows]: the rows' log probabilities.
+ */
+int pgc_policy_loss(const pgc_logits *z, int32_t reduction, int64_t sequences, const int32_t *offsets,
+                    const float *old_logp, const float *advantage, const float *ref_logp, float clip_low,
+                    float clip_high, float kl, float scale, float *loss, float *terms, float *logp, void *workspace,
+                    int64_t workspace_bytes, void *stream);
+
+/* pgc_balance_workspace — bytes of workspace of pgc_balance_loss. Errors: PGC_EINVAL. */
+int pgc_balance_workspace(int64_t rows, int64_t experts, int64_t *bytes);
+
+/*
+ * pgc_balance_loss — a router's choice, its counts and its balance loss.  Rows
+ * of `experts` logits (dtype, ld as in pgc_logits); n rows have mask[t] != 0 (all,
+ * if mask is NULL).  With p = softmax of a row (temperature 1) and the counts c,
+ *   loss = alpha experts / (k n^2) sum_e c_e sum_t p_te,
+ * whose gradient takes the counts as constants.
+ *   choice : [rows][k].  given = 0: receives the experts of each row's k largest
+ *     logits, largest first, ties to the lower expert; -1 in a row that takes no
+ *     part, and where fewer than k logits are above -inf.  given != 0: read; entries outside
+ *     [0, experts) count for no expert, the same expert twice counts twice.
+ *   counts : [experts] times each expert was chosen by rows that take part.
+ *   grad   : as in pgc_logits (NULL: only the loss); zeros for rows that take
+ *     no part.  A row all of whose logits are -inf adds nothing and gets zeros.
+ *   loss   : [1], 0 if n = 0.
+ * Errors: as above; PGC_ENOTSUP for more than 1024 experts or k > 64.
+ */
+int pgc_balance_loss(int32_t dtype, int64_t rows, int64_t experts, const void *logits, int64_t ld, const uint8_t *mask,
+                     int32_t k, int32_t given, int32_t *choice, float alpha, float *loss, int32_t *counts, void *grad,
+                     int64_t grad_ld, void *workspace, int64_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

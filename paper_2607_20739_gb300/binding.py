@@ -33,12 +33,20 @@ SCHEMES = {"FR": FR, "CR": CR}
 LOSSES = {"logistic": LOGISTIC, "lsq": LSQ, "softmax": SOFTMAX}
 DTYPES = {"f32": F32, "bf16": BF16}
 MODE_PGC, MODE_IS_SGD, MODE_GC, MODE_NAIVE_CR = 0, 1, 2, 3
+PREFERENCES = {"sigmoid": 0, "hinge": 1, "squared": 2}
+REDUCTIONS = {"tokens": 0, "sequences": 1, "sum": 2}
 MODES = {"pgc": MODE_PGC, "is_sgd": MODE_IS_SGD, "gc": MODE_GC, "naive_cr": MODE_NAIVE_CR}
 
 
 class StepInfo(C.Structure):
     _fields_ = [("t", C.c_int64), ("slot", C.c_int32), ("received", C.c_int32),
                 ("eval_partition", C.POINTER(C.c_int32)), ("fr_rep", C.POINTER(C.c_int32))]
+
+
+class Logits(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("target", C.c_void_p), ("grad", C.c_void_p), ("rows", C.c_int64),
+                ("classes", C.c_int64), ("ld", C.c_int64), ("grad_ld", C.c_int64), ("dtype", C.c_int32),
+                ("temperature", C.c_float)]
 
 
 _vp = C.c_void_p
@@ -74,6 +82,16 @@ _sig = {
     "pgc_timing": (C.c_int, [_vp, _i32]),
     "pgc_timing_read": (C.c_int, [_vp, C.POINTER(C.c_double), C.POINTER(_i64), C.POINTER(_i64)]),
     "pgc_gradient_noalloc": (C.c_int, [_i32, _i32, _i64, _i64, _vp, _vp, _vp, _vp, _vp]),
+    "pgc_loss_workspace": (C.c_int, [_i64, _i64, C.POINTER(_i64)]),
+    "pgc_token_logprob": (C.c_int, [C.POINTER(Logits), _vp, _vp, _vp]),
+    "pgc_token_logprob_grad": (C.c_int, [C.POINTER(Logits), _vp, _vp, _vp]),
+    "pgc_preference_loss": (C.c_int, [C.POINTER(Logits), _i32, _i64, _vp, _vp, C.c_float, C.c_float, C.c_float, _i32,
+                                      C.c_float, _vp, _vp, _vp, _i64, _vp]),
+    "pgc_policy_loss": (C.c_int, [C.POINTER(Logits), _i32, _i64, _vp, _vp, _vp, _vp, C.c_float, C.c_float, C.c_float,
+                                  C.c_float, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "pgc_balance_workspace": (C.c_int, [_i64, _i64, C.POINTER(_i64)]),
+    "pgc_balance_loss": (C.c_int, [_i32, _i64, _i64, _vp, _i64, _vp, _i32, _i32, _vp, C.c_float, _vp, _vp, _vp, _i64,
+                                   _vp, _i64, _vp]),
 }
 for _name, (_res, _args) in _sig.items():
     _f = getattr(lib, _name)

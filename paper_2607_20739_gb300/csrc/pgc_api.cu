@@ -636,6 +636,8 @@ int copy_out(pgc_ctx* ctx, float* dst, const float* src, int on_device) {
 
 }  // namespace
 
+int pgc::report_cuda(cudaError_t e) { return cuda_fail(nullptr, e); }
+
 extern "C" {
 
 const char* pgc_gradient_path(const pgc_ctx* ctx) {

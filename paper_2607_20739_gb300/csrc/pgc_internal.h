@@ -434,5 +434,7 @@ bool make_tmap_2d(void* tm_out, bool f32, const void* base, uint64_t inner, uint
 
 // ---- misc -------------------------------------------------------------------
 cudaError_t launch_f32_to_bf16(const float* src, uint16_t* dst, int64_t count, cudaStream_t st);
+// The status code of a CUDA error in a call without a context; keeps its name for pgc_last_cuda_error.
+int report_cuda(cudaError_t e);
 
 }  // namespace pgc
