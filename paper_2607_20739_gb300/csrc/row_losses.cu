@@ -9,54 +9,32 @@
 #include <algorithm>
 #include <cmath>
 
-#include "dev_common.cuh"
 #include "pgc.h"
 #include "pgc_internal.h"
+#include "row_slice.cuh"
 
 namespace pgc {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kUnroll = 4;            // 16-byte pieces a thread has in flight
+constexpr int kMaxCluster = 8;
 
 struct Rows {
   const void* x;
   void* g;
   const int32_t* y;
   int64_t T, V, ld, ldg;
-  float inv_tau;
+  float inv_tau, c;                   // 1 / tau, log2(e) / tau
 };
 
-__device__ __forceinline__ float to_float(float v) { return v; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ void put(float* p, float v) { *p = v; }
-__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
-
-__device__ float block_max(float v, float* red) {
-  v = warp_max(v);
-  __syncthreads();
-  if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = v;
-  __syncthreads();
-  v = red[0];
-  for (int i = 1; i < kThreads / 32; ++i) v = fmaxf(v, red[i]);
-  return v;
-}
-__device__ float block_sum(float v, float* red) {
-  v = warp_sum(v);
-  __syncthreads();
-  if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = v;
-  __syncthreads();
-  v = 0.f;
-  for (int i = 0; i < kThreads / 32; ++i) v += red[i];
-  return v;
-}
 __device__ double block_sum_f64(double v, double* red) {
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   __syncthreads();
   if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = v;
   __syncthreads();
   v = 0.0;
-  for (int i = 0; i < kThreads / 32; ++i) v += red[i];
+  for (int i = 0; i < kWarps; ++i) v += red[i];
   return v;
 }
 
@@ -66,54 +44,123 @@ struct Head {
   int32_t bad;        // offsets that fall, or leave [0, T]
 };
 
-// One CTA per row: largest logit, log of the sum, target's log probability.
-template <typename E>
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+__device__ __forceinline__ int cluster_ranks() {
+  int n;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+  return n;
+}
+__device__ __forceinline__ int cluster_rank() {
+  int n;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(n));
+  return n;
+}
+
+// A row belongs to a warp (G = 32), or to the CTA, or the cluster of CTAs, of
+// the group's threads.  Exchanges alternate between two buffers, so that one
+// barrier each is enough.
+struct Shared {
+  float2 part[2][kWarps];
+  float2 cta[2][kMaxCluster];
+};
+template <int G>
+__device__ __forceinline__ Online merge(Online o, float c, Shared& sh, int& turn, int rank, int ranks) {
+  o = warp_merge(o, c);
+  if (G == 32) return o;
+  const int lane = threadIdx.x % 32, b = turn++ & 1;
+  if (lane == 0) sh.part[b][threadIdx.x / 32] = make_float2(o.m, o.s);
+  __syncthreads();
+  Online q;
+  if (lane < kWarps) {
+    q.m = sh.part[b][lane].x;
+    q.s = sh.part[b][lane].y;
+    q.M = ref_of(q.m, c);
+  }
+  o = warp_merge(q, c);
+  if (ranks == 1) return o;
+  if (threadIdx.x < ranks) {
+    uint32_t at;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(&sh.cta[b][rank])), "r"((uint32_t)threadIdx.x));
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(o.m), "f"(o.s) : "memory");
+  }
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  q = Online();
+  if (lane < ranks) {
+    q.m = sh.cta[b][lane].x;
+    q.s = sh.cta[b][lane].y;
+    q.M = ref_of(q.m, c);
+  }
+  return warp_merge(q, c);
+}
+
+// The row's largest logit and log sum, for all threads of the group.
+template <typename E, int G>
+__device__ __forceinline__ float2 row_stats(const E* x, const Slice& s, int tid, float c, Shared& sh, int& turn,
+                                            int rank, int ranks) {
+  Online o = merge<G>(slice_stats<E, G, kUnroll>(x, s, tid, c), c, sh, turn, rank, ranks);
+  if (!is_extreme(o.m, c)) return make_float2(o.m, logf(o.s) - kLn2 * fmaf(o.m, c, -o.M));
+  Online q;
+  q.M = 0.f;
+  for (int v = s.first + tid; v < s.last; v += G) q.s += exp2f((Elem<E>::get(x + v) - o.m) * c);
+  q.m = 0.f;
+  return make_float2(o.m, logf(merge<G>(q, c, sh, turn, rank, ranks).s));
+}
+
+__device__ __forceinline__ float target_logp(float xy, float2 st, const Rows& a) {
+  return (xy - st.x) * a.inv_tau - st.y;
+}
+
+// One row per group: largest logit, log of the sum, target's log probability.
+template <typename E, int G>
 __global__ void __launch_bounds__(kThreads) row_stats_kernel(Rows a, float* logp, float2* stats, Head* head) {
-  __shared__ float red[kThreads / 32];
-  const int64_t t = blockIdx.x;
-  if (head && t == 0 && threadIdx.x == 0) *head = Head{0, 0};
+  __shared__ Shared sh;
+  const int rank = G == 32 ? 0 : cluster_rank(), ranks = G == 32 ? 1 : cluster_ranks();
+  const int tid = threadIdx.x % G;
+  const int64_t t = G == 32 ? blockIdx.x * (int64_t)kWarps + threadIdx.x / 32 : blockIdx.x / ranks;
+  let_next_start();
+  if (head && blockIdx.x == 0 && threadIdx.x == 0) *head = Head{0, 0};
+  if (t >= a.T) return;
   const int32_t y = a.y[t];
   if (y < 0) {
-    if (threadIdx.x == 0) {
+    if (tid == 0 && rank == 0) {
       logp[t] = 0.f;
       stats[t] = make_float2(0.f, 0.f);
     }
     return;
   }
   const E* x = static_cast<const E*>(a.x) + t * a.ld;
-  float m = -INFINITY;
-  for (int64_t v = threadIdx.x; v < a.V; v += kThreads) m = fmaxf(m, to_float(x[v]));
-  m = block_max(m, red);
-  const float c = a.inv_tau * kLog2e;
-  float s = 0.f;
-  for (int64_t v = threadIdx.x; v < a.V; v += kThreads) s += exp2f((to_float(x[v]) - m) * c);
-  s = block_sum(s, red);
-  if (threadIdx.x == 0) {
-    const float L = logf(s);
-    logp[t] = y < a.V ? (to_float(x[y]) - m) * a.inv_tau - L : NAN;
-    stats[t] = make_float2(m, L);
+  const float xy = y < a.V ? Elem<E>::get(x + y) : NAN;
+  int turn = 0;
+  const float2 st = row_stats<E, G>(x, slice_of(x, (int)a.V, rank, ranks), tid, a.c, sh, turn, rank, ranks);
+  if (tid == 0 && rank == 0) {
+    logp[t] = target_logp(xy, st, a);
+    stats[t] = st;
   }
 }
 
-template <typename E>
+template <typename E, int G>
 __global__ void __launch_bounds__(kThreads) row_grad_kernel(Rows a, const float* coef, const float2* stats,
                                                             const Head* head) {
-  const int64_t t = blockIdx.x;
+  const int rank = G == 32 ? 0 : cluster_rank(), ranks = G == 32 ? 1 : cluster_ranks();
+  const int tid = threadIdx.x % G;
+  const int64_t t = G == 32 ? blockIdx.x * (int64_t)kWarps + threadIdx.x / 32 : blockIdx.x / ranks;
+  if (t >= a.T) return;
   const int32_t y = a.y[t];
   E* g = static_cast<E*>(a.g) + t * a.ldg;
+  const E* x = static_cast<const E*>(a.x) + t * a.ld;
+  const Slice s = slice_of(x, (int)a.V, rank, ranks);
+  if (head) wait_for_previous();
   const bool bad = head && head->bad;
-  if (y < 0 && !bad) {
-    for (int64_t v = threadIdx.x; v < a.V; v += kThreads) put(g + v, 0.f);
+  const float k = bad || y >= a.V ? NAN : y < 0 ? 0.f : coef[t];
+  if (k == 0.f || isnan(k)) {
+    slice_fill<E, G>(g, s.first, s.last, tid, k);
     return;
   }
-  const E* x = static_cast<const E*>(a.x) + t * a.ld;
-  const float k = (bad || y >= a.V ? NAN : coef[t]) * a.inv_tau;
-  const float2 st = bad ? make_float2(0.f, 0.f) : stats[t];
-  const float c = a.inv_tau * kLog2e, l2 = st.y * kLog2e;
-  for (int64_t v = threadIdx.x; v < a.V; v += kThreads) {
-    const float p = exp2f((to_float(x[v]) - st.x) * c - l2);
-    put(g + v, k == 0.f ? 0.f : k * ((v == y ? 1.f : 0.f) - p));
-  }
+  const float2 st = stats[t];
+  slice_grad<E, G, kUnroll>(x, g, s, tid, row_grad(st.x, st.y, k, a.inv_tau, a.c, y));
 }
 
 // ---- preference ------------------------------------------------------------
@@ -153,9 +200,11 @@ __device__ double pref_loss(const Pref& a, double gap, double* slope) {
 }
 
 __global__ void __launch_bounds__(kThreads) pair_kernel(Pref a) {
-  __shared__ double red[kThreads / 32];
+  __shared__ double red[kWarps];
   __shared__ int last;
   const int64_t i = blockIdx.x;
+  let_next_start();
+  wait_for_previous();
   if (i < a.pairs) {
     int64_t at[3];
     bool bad = false;
@@ -233,7 +282,7 @@ struct Policy {
 
 // Rows with a target (tokens), or sequences with one and 1 / their rows (sequences).
 __global__ void __launch_bounds__(kThreads) count_kernel(Policy a) {
-  __shared__ double red[kThreads / 32];
+  __shared__ double red[kWarps];
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.head = Head{0, 0};
   double total = 0.0;
   if (a.reduction == PGC_MEAN_SEQUENCES) {
@@ -264,7 +313,7 @@ __global__ void __launch_bounds__(kThreads) count_kernel(Policy a) {
 }
 
 __global__ void __launch_bounds__(kThreads) policy_kernel(Policy a) {
-  __shared__ double red[kThreads / 32];
+  __shared__ double red[kWarps];
   __shared__ int last;
   double n = 0.0;
   bool bad = false;
@@ -338,27 +387,76 @@ int check_rows(const pgc_logits* z, bool grad_required) {
 }
 
 Rows rows_of(const pgc_logits* z) {
-  return Rows{z->x, z->grad, z->target, z->rows, z->classes, z->ld, z->grad_ld, 1.f / z->temperature};
+  const float inv_tau = 1.f / z->temperature;
+  return Rows{z->x, z->grad, z->target, z->rows, z->classes, z->ld, z->grad_ld, inv_tau, inv_tau * kLog2e};
+}
+
+int sm_count() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return 148;
+  return n;
+}
+
+// How a call's rows lie on the grid: a warp each (short rows), a CTA each, or
+// a cluster each (few long rows).
+constexpr int64_t kWarpRowBytes = 4096;
+struct Shape {
+  bool warp;
+  int ranks;
+  unsigned grid;
+};
+Shape shape_of(const pgc_logits* z) {
+  const int64_t bytes = z->classes * (z->dtype == PGC_BF16 ? 2 : 4);
+  Shape s{bytes <= kWarpRowBytes, 1, 0};
+  if (s.warp) {
+    s.grid = (unsigned)((z->rows + kWarps - 1) / kWarps);
+    return s;
+  }
+  const int64_t sms = sm_count();
+  while (s.ranks < kMaxCluster && z->rows * s.ranks * 2 <= 2 * sms && bytes / (s.ranks * 2) >= kWarpRowBytes) s.ranks *= 2;
+  s.grid = (unsigned)(z->rows * s.ranks);
+  return s;
+}
+
+template <typename... P, typename... A>
+cudaError_t launch(void (*kernel)(P...), unsigned grid, int ranks, bool pdl, cudaStream_t st, A... args) {
+  cudaLaunchAttribute attr[2];
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = st;
+  cfg.attrs = attr;
+  if (ranks > 1) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+    attr[cfg.numAttrs].val.clusterDim.x = (unsigned)ranks;
+    attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
+    ++cfg.numAttrs;
+  }
+  if (pdl) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+    ++cfg.numAttrs;
+  }
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
 }
 
 cudaError_t launch_stats(const pgc_logits* z, float* logp, float2* stats, Head* head, cudaStream_t st) {
   if (z->rows == 0) return cudaSuccess;
-  const Rows a = rows_of(z);
-  if (z->dtype == PGC_BF16)
-    row_stats_kernel<__nv_bfloat16><<<(unsigned)z->rows, kThreads, 0, st>>>(a, logp, stats, head);
-  else
-    row_stats_kernel<float><<<(unsigned)z->rows, kThreads, 0, st>>>(a, logp, stats, head);
-  return cudaGetLastError();
+  const Shape s = shape_of(z);
+  const bool half = z->dtype == PGC_BF16;
+  return launch(half ? s.warp ? row_stats_kernel<__nv_bfloat16, 32> : row_stats_kernel<__nv_bfloat16, kThreads>
+                     : s.warp ? row_stats_kernel<float, 32> : row_stats_kernel<float, kThreads>,
+                s.grid, s.ranks, false, st, rows_of(z), logp, stats, head);
 }
 
 cudaError_t launch_grad(const pgc_logits* z, const float* coef, const float2* stats, const Head* head, cudaStream_t st) {
   if (z->rows == 0) return cudaSuccess;
-  const Rows a = rows_of(z);
-  if (z->dtype == PGC_BF16)
-    row_grad_kernel<__nv_bfloat16><<<(unsigned)z->rows, kThreads, 0, st>>>(a, coef, stats, head);
-  else
-    row_grad_kernel<float><<<(unsigned)z->rows, kThreads, 0, st>>>(a, coef, stats, head);
-  return cudaGetLastError();
+  const Shape s = shape_of(z);
+  const bool half = z->dtype == PGC_BF16;
+  return launch(half ? s.warp ? row_grad_kernel<__nv_bfloat16, 32> : row_grad_kernel<__nv_bfloat16, kThreads>
+                     : s.warp ? row_grad_kernel<float, 32> : row_grad_kernel<float, kThreads>,
+                s.grid, s.ranks, head != nullptr, st, rows_of(z), coef, stats, head);
 }
 
 constexpr int kMaxParts = 1024;       // CTAs of the kernels that leave partial sums
@@ -447,8 +545,7 @@ int pgc_preference_loss(const pgc_logits *z, int32_t kind, int64_t pairs, const 
   if (e != cudaSuccess) return report_cuda(e);
   Pref a{kind, average, pairs, z->rows, offsets, z->target, ref_logp, w.logp, beta, margin, smoothing, scale,
          w.coef, logp, w.part, loss, w.head};
-  pair_kernel<<<(unsigned)std::max<int64_t>(pairs, 1), kThreads, 0, st>>>(a);
-  e = cudaGetLastError();
+  e = launch(pair_kernel, (unsigned)std::max<int64_t>(pairs, 1), 1, true, st, a);
   if (e == cudaSuccess && z->grad) e = launch_grad(z, w.coef, w.stats, w.head, st);
   return report_cuda(e);
 }
