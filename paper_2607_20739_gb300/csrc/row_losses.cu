@@ -17,6 +17,7 @@ namespace pgc {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMaxWarps = 32;
 constexpr int kUnroll = 4;            // 16-byte pieces a thread has in flight
 constexpr int kMaxCluster = 8;
 
@@ -24,17 +25,53 @@ struct Rows {
   const void* x;
   void* g;
   const int32_t* y;
-  int64_t T, V, ld, ldg;
+  int64_t T, ld, ldg;
+  int32_t V;
   float inv_tau, c;                   // 1 / tau, log2(e) / tau
 };
 
-__device__ double block_sum_f64(double v, double* red) {
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+// A sum with its rounding errors kept beside it (two-sum): the double unit is
+// slow enough here to hold up a row.
+struct Sum {
+  float s = 0.f, e = 0.f;
+  __device__ void add(float v) {
+    const float t = s + v, b = t - s;
+    e += (s - (t - b)) + (v - b);
+    s = t;
+  }
+  __device__ void add(const Sum& o) {
+    add(o.s);
+    e += o.e;
+  }
+  // infinities leave no error behind
+  __device__ float value() const { return isfinite(s) ? s + e : s; }
+  __device__ double value_f64() const { return isfinite(s) ? (double)s + e : s; }
+};
+
+__device__ __forceinline__ Sum shuffle_down(const Sum& v, int o) {
+  Sum q;
+  q.s = __shfl_down_sync(0xffffffffu, v.s, o);
+  q.e = __shfl_down_sync(0xffffffffu, v.e, o);
+  return q;
+}
+// The block's sum, in thread 0.
+__device__ Sum block_sum(Sum v, Sum* red) {
+  for (int o = 16; o > 0; o >>= 1) v.add(shuffle_down(v, o));
   __syncthreads();
   if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = v;
   __syncthreads();
-  v = 0.0;
-  for (int i = 0; i < kWarps; ++i) v += red[i];
+  if (threadIdx.x == 0)
+    for (int i = 1; i < (int)blockDim.x / 32; ++i) v.add(red[i]);
+  return v;
+}
+// The block's sum, in all threads.
+__device__ int block_sum(int v, int* red) {
+  v = __reduce_add_sync(0xffffffffu, v);
+  __syncthreads();
+  if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = v;
+  __syncthreads();
+  v = 0;
+  for (int i = 0; i < (int)blockDim.x / 32; ++i) v += red[i];
   return v;
 }
 
@@ -62,7 +99,7 @@ __device__ __forceinline__ int cluster_rank() {
 // the group's threads.  Exchanges alternate between two buffers, so that one
 // barrier each is enough.
 struct Shared {
-  float2 part[2][kWarps];
+  float2 part[2][kMaxWarps];
   float2 cta[2][kMaxCluster];
 };
 template <int G>
@@ -73,7 +110,7 @@ __device__ __forceinline__ Online merge(Online o, float c, Shared& sh, int& turn
   if (lane == 0) sh.part[b][threadIdx.x / 32] = make_float2(o.m, o.s);
   __syncthreads();
   Online q;
-  if (lane < kWarps) {
+  if (lane < G / 32) {
     q.m = sh.part[b][lane].x;
     q.s = sh.part[b][lane].y;
     q.M = ref_of(q.m, c);
@@ -85,6 +122,7 @@ __device__ __forceinline__ Online merge(Online o, float c, Shared& sh, int& turn
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(&sh.cta[b][rank])), "r"((uint32_t)threadIdx.x));
     asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(o.m), "f"(o.s) : "memory");
   }
+  __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   q = Online();
@@ -134,7 +172,7 @@ __global__ void __launch_bounds__(kThreads) row_stats_kernel(Rows a, float* logp
   const E* x = static_cast<const E*>(a.x) + t * a.ld;
   const float xy = y < a.V ? Elem<E>::get(x + y) : NAN;
   int turn = 0;
-  const float2 st = row_stats<E, G>(x, slice_of(x, (int)a.V, rank, ranks), tid, a.c, sh, turn, rank, ranks);
+  const float2 st = row_stats<E, G>(x, slice_of(x, a.V, rank, ranks), tid, a.c, sh, turn, rank, ranks);
   if (tid == 0 && rank == 0) {
     logp[t] = target_logp(xy, st, a);
     stats[t] = st;
@@ -151,7 +189,7 @@ __global__ void __launch_bounds__(kThreads) row_grad_kernel(Rows a, const float*
   const int32_t y = a.y[t];
   E* g = static_cast<E*>(a.g) + t * a.ldg;
   const E* x = static_cast<const E*>(a.x) + t * a.ld;
-  const Slice s = slice_of(x, (int)a.V, rank, ranks);
+  const Slice s = slice_of(x, a.V, rank, ranks);
   if (head) wait_for_previous();
   const bool bad = head && head->bad;
   const float k = bad || y >= a.V ? NAN : y < 0 ? 0.f : coef[t];
@@ -160,7 +198,7 @@ __global__ void __launch_bounds__(kThreads) row_grad_kernel(Rows a, const float*
     return;
   }
   const float2 st = stats[t];
-  slice_grad<E, G, kUnroll>(x, g, s, tid, row_grad(st.x, st.y, k, a.inv_tau, a.c, y));
+  slice_grad<E, G, kUnroll>(x, g, s, tid, Elem<E>::get(x + y), row_grad(st.x, st.y, k, a.inv_tau, a.c, y));
 }
 
 // ---- preference ------------------------------------------------------------
@@ -175,70 +213,93 @@ struct Pref {
   float beta, margin, smoothing, scale;
   float* coef;          // [T]
   float* seq;           // [pairs][2] out
-  double* pair_loss;    // [pairs]
+  float* pair_loss;     // [pairs]
   float* loss;
   Head* head;
 };
 
-// loss and its derivative of one pair's gap of log ratios
-__device__ double pref_loss(const Pref& a, double gap, double* slope) {
-  const double beta = a.beta, e = a.smoothing;
-  gap -= (double)a.margin / beta;
-  const double h = beta * gap;
+// Loss of one pair's gap of log ratios, and its derivative.
+__device__ float pref_loss(const Pref& a, float gap, float* slope) {
+  const float beta = a.beta, e = a.smoothing;
+  const float h = beta * gap;
   if (a.kind == PGC_PREF_SIGMOID) {
-    const double soft = log1p(exp(-fabs(h)));
-    *slope = beta * (1.0 / (1.0 + exp(-h)) - (1.0 - e));
-    return (1.0 - e) * (soft + fmax(-h, 0.0)) + e * (soft + fmax(h, 0.0));
+    const float soft = log1pf(expf(-fabsf(h)));
+    *slope = beta * (1.f / (1.f + expf(-h)) - (1.f - e));
+    return (1.f - e) * (soft + (isnan(h) ? h : fmaxf(-h, 0.f))) + e * (soft + fmaxf(h, 0.f));
   }
   if (a.kind == PGC_PREF_HINGE) {
-    *slope = beta * ((h > -1.0 ? e : 0.0) - (h < 1.0 ? 1.0 - e : 0.0));
-    return (1.0 - e) * fmax(1.0 - h, 0.0) + e * fmax(1.0 + h, 0.0);
+    *slope = beta * ((h > -1.f ? e : 0.f) - (h < 1.f ? 1.f - e : 0.f)) + (isnan(h) ? h : 0.f);
+    return (1.f - e) * fmaxf(1.f - h, 0.f) + e * fmaxf(1.f + h, 0.f) + (isnan(h) ? h : 0.f);
   }
-  const double up = gap - 0.5 / beta, down = gap + 0.5 / beta;
-  *slope = 2.0 * ((1.0 - e) * up + e * down);
-  return (1.0 - e) * up * up + e * down * down;
+  const float up = gap - 0.5f / beta, down = gap + 0.5f / beta;
+  *slope = 2.f * ((1.f - e) * up + e * down);
+  return (1.f - e) * up * up + e * down * down;
+}
+
+// A pair's scores, loss and coefficients from its rows' log probabilities:
+// the CTA's work, the results in thread 0.
+struct PairWork {
+  Sum red[kMaxWarps];
+  int count[kMaxWarps];
+};
+__device__ float2 finish_pair(const Pref& a, int64_t i, const int32_t (&at)[3], PairWork& sh) {
+  Sum score[2];
+  int n[2];
+  for (int j = 0; j < 2; ++j) {
+    Sum s;
+    int m = 0;
+    for (int64_t t = at[j] + (int64_t)threadIdx.x; t < at[j + 1]; t += blockDim.x)
+      if (a.y[t] >= 0) {
+        s.add(__ldcg(a.logp + t));
+        ++m;
+      }
+    n[j] = max(block_sum(m, sh.count), 1);
+    score[j] = block_sum(s, sh.red);
+  }
+  float2 coef = make_float2(0.f, 0.f);
+  if (threadIdx.x == 0) {
+    double v[2], gap;
+    for (int j = 0; j < 2; ++j) {
+      v[j] = score[j].value_f64() / (a.average ? n[j] : 1);
+      a.seq[2 * i + j] = (float)v[j];
+    }
+    gap = v[0] - v[1] - (double)a.margin / a.beta;
+    if (a.ref) gap -= (double)a.ref[2 * i] - (double)a.ref[2 * i + 1];
+    float slope;
+    a.pair_loss[i] = pref_loss(a, (float)gap, &slope);
+    slope = slope * a.scale / (float)a.pairs;
+    coef = make_float2(slope / (a.average ? n[0] : 1), -slope / (a.average ? n[1] : 1));
+  }
+  return coef;
+}
+// The mean of the pairs' losses.
+__device__ void finish_loss(const Pref& a, bool bad, PairWork& sh) {
+  Sum s;
+  for (int64_t j = threadIdx.x; j < a.pairs; j += blockDim.x) s.add(__ldcg(a.pair_loss + j));
+  s = block_sum(s, sh.red);
+  if (threadIdx.x == 0) *a.loss = bad ? NAN : a.pairs ? (float)(s.value_f64() * a.scale / (double)a.pairs) : 0.f;
 }
 
 __global__ void __launch_bounds__(kThreads) pair_kernel(Pref a) {
-  __shared__ double red[kWarps];
+  __shared__ PairWork sh;
+  __shared__ float2 coef;
   __shared__ int last;
   const int64_t i = blockIdx.x;
   let_next_start();
   wait_for_previous();
   if (i < a.pairs) {
-    int64_t at[3];
-    bool bad = false;
-    for (int j = 0; j < 3; ++j) {
-      at[j] = a.off[2 * i + j];
-      bad |= at[j] < 0 || at[j] > a.T || (j && at[j] < at[j - 1]);
-    }
-    double score[2] = {0.0, 0.0}, n[2] = {0.0, 0.0};
-    if (!bad)
-      for (int j = 0; j < 2; ++j) {
-        double s = 0.0, m = 0.0;
-        for (int64_t t = at[j] + threadIdx.x; t < at[j + 1]; t += kThreads)
-          if (a.y[t] >= 0) {
-            s += a.logp[t];
-            m += 1.0;
-          }
-        n[j] = fmax(block_sum_f64(m, red), 1.0);
-        score[j] = block_sum_f64(s, red) / (a.average ? n[j] : 1.0);
+    const int32_t at[3] = {a.off[2 * i], a.off[2 * i + 1], a.off[2 * i + 2]};
+    const bool bad = at[0] < 0 || at[1] < at[0] || at[2] < at[1] || at[2] > a.T;
+    if (bad) {
+      if (threadIdx.x == 0) {
+        a.seq[2 * i] = a.seq[2 * i + 1] = NAN;
+        atomicOr(&a.head->bad, 1);
       }
-    double gap = score[0] - score[1];
-    if (a.ref) gap -= (double)a.ref[2 * i] - (double)a.ref[2 * i + 1];
-    double slope;
-    const double loss = pref_loss(a, gap, &slope);
-    slope *= (double)a.scale / (double)a.pairs;
-    if (!bad)
-      for (int j = 0; j < 2; ++j) {
-        const float c = (float)((j ? -slope : slope) / (a.average ? n[j] : 1.0));
-        for (int64_t t = at[j] + threadIdx.x; t < at[j + 1]; t += kThreads) a.coef[t] = c;
-      }
-    if (threadIdx.x == 0) {
-      a.seq[2 * i] = bad ? NAN : (float)score[0];
-      a.seq[2 * i + 1] = bad ? NAN : (float)score[1];
-      a.pair_loss[i] = loss;
-      if (bad) atomicOr(&a.head->bad, 1);
+    } else {
+      const float2 c = finish_pair(a, i, at, sh);
+      if (threadIdx.x == 0) coef = c;
+      __syncthreads();
+      for (int64_t t = at[0] + (int64_t)threadIdx.x; t < at[2]; t += kThreads) a.coef[t] = t < at[1] ? coef.x : coef.y;
     }
   }
   // rows outside every sequence
@@ -251,14 +312,7 @@ __global__ void __launch_bounds__(kThreads) pair_kernel(Pref a) {
   __syncthreads();
   if (threadIdx.x == 0) last = atomic_add_acq_rel(&a.head->ticket, 1) == (int)gridDim.x - 1;
   __syncthreads();
-  if (!last) return;
-  double s = 0.0;
-  for (int64_t j = threadIdx.x; j < a.pairs; j += kThreads) s += __ldcg(a.pair_loss + j);
-  s = block_sum_f64(s, red);
-  if (threadIdx.x == 0) {
-    const bool bad = *(volatile int32_t*)&a.head->bad != 0;
-    *a.loss = bad ? NAN : a.pairs ? (float)(s * a.scale / (double)a.pairs) : 0.f;
-  }
+  if (last) finish_loss(a, *(volatile int32_t*)&a.head->bad != 0, sh);
 }
 
 // ---- policy ------------------------------------------------------------------
@@ -269,34 +323,35 @@ struct Policy {
   const int32_t* off;
   const int32_t* y;
   const float *old_logp, *ref_logp, *advantage;
-  const float* logp;
+  float* logp;
   float low, high, kl, scale;
-  float* coef;          // [T]
   int32_t* count;       // [grid of the count kernel]: rows with a target, or sequences that have one
   int counts;
   float* share;         // [T]: 1 / rows with a target in the row's sequence
-  double* part;         // [grid][3]
+  float2* part;         // [grid][3]
   float *loss, *terms;
   Head* head;
 };
 
 // Rows with a target (tokens), or sequences with one and 1 / their rows (sequences).
 __global__ void __launch_bounds__(kThreads) count_kernel(Policy a) {
-  __shared__ double red[kWarps];
+  __shared__ int red[kWarps];
+  let_next_start();
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.head = Head{0, 0};
-  double total = 0.0;
+  int total = 0;
+  bool bad = false;
   if (a.reduction == PGC_MEAN_SEQUENCES) {
     for (int64_t s = blockIdx.x; s < a.S; s += gridDim.x) {
       const int64_t lo = a.off[s], hi = a.off[s + 1];
-      const bool bad = lo < 0 || hi < lo || hi > a.T;
-      double n = 0.0;
-      if (!bad)
-        for (int64_t t = lo + threadIdx.x; t < hi; t += kThreads) n += a.y[t] >= 0;
-      n = block_sum_f64(n, red);
-      if (n > 0.0) total += 1.0;
-      if (!bad)
-        for (int64_t t = lo + threadIdx.x; t < hi; t += kThreads) a.share[t] = (float)(1.0 / fmax(n, 1.0));
-      if (bad) total = NAN;
+      if (lo < 0 || hi < lo || hi > a.T) {
+        bad = true;
+        continue;
+      }
+      int n = 0;
+      for (int64_t t = lo + threadIdx.x; t < hi; t += kThreads) n += a.y[t] >= 0;
+      n = block_sum(n, red);
+      total += n > 0;
+      for (int64_t t = lo + threadIdx.x; t < hi; t += kThreads) a.share[t] = 1.f / (float)max(n, 1);
     }
     if (blockIdx.x == 0) {
       const int64_t end = a.S ? min((int64_t)max(a.off[0], 0), a.T) : a.T;
@@ -307,65 +362,317 @@ __global__ void __launch_bounds__(kThreads) count_kernel(Policy a) {
   } else {
     for (int64_t t = blockIdx.x * (int64_t)kThreads + threadIdx.x; t < a.T; t += gridDim.x * (int64_t)kThreads)
       total += a.y[t] >= 0;
-    total = block_sum_f64(total, red);
+    total = block_sum(total, red);
   }
-  if (threadIdx.x == 0) a.count[blockIdx.x] = total >= 0.0 ? (int32_t)total : -1;
+  if (threadIdx.x == 0) a.count[blockIdx.x] = bad ? -1 : total;
 }
 
-__global__ void __launch_bounds__(kThreads) policy_kernel(Policy a) {
-  __shared__ double red[kWarps];
-  __shared__ int last;
-  double n = 0.0;
+// A row's inputs besides its logits, read a row ahead (its target two rows).
+struct RowIn {
+  int32_t y;
+  float xy, advantage, old, ref, share;
+};
+template <typename E>
+__device__ __forceinline__ RowIn row_in(const Rows& a, const Policy& p, int64_t t, int32_t y) {
+  RowIn r{y, 0.f, 0.f, 0.f, 0.f, 1.f};
+  if (y < 0) return r;
+  r.xy = y < a.V ? Elem<E>::get(static_cast<const E*>(a.x) + t * a.ld + y) : NAN;
+  r.advantage = p.advantage[t];
+  r.old = p.old_logp[t];
+  if (p.ref_logp) r.ref = p.ref_logp[t];
+  if (p.reduction == PGC_MEAN_SEQUENCES) r.share = p.share[t];
+  return r;
+}
+
+// The scalars of the policy loss: the rows' weights, of the counts that the
+// kernel before has taken, a row's part of the sums and its coefficient.
+struct PolicyState {
+  Sum sum[3];        // term, KL, clipped
   bool bad = false;
-  for (int i = 0; i < a.counts; ++i) {
-    bad |= a.count[i] < 0;
-    n += a.count[i];
+  float w0 = 1.f;
+
+  __device__ void weigh(const Policy& p) {
+    wait_for_previous();
+    int n = 0;
+    for (int i = threadIdx.x % 32; i < p.counts; i += 32) {
+      const int q = p.count[i];
+      bad |= q < 0;
+      n += q;
+    }
+    bad = __any_sync(0xffffffffu, bad);
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (p.reduction != PGC_SUM) w0 = 1.f / (float)max(n, 1);
   }
-  const float w0 = a.reduction == PGC_SUM ? 1.f : (float)(1.0 / fmax(n, 1.0));
-  double term = 0.0, klsum = 0.0, clipped = 0.0;
-  for (int64_t t = blockIdx.x * (int64_t)kThreads + threadIdx.x; t < a.T; t += gridDim.x * (int64_t)kThreads) {
-    if (a.y[t] < 0 || bad) {
-      a.coef[t] = bad ? NAN : 0.f;
-      continue;
-    }
-    const float w = a.reduction == PGC_MEAN_SEQUENCES ? w0 * a.share[t] : w0;
-    if (w == 0.f) {
-      a.coef[t] = 0.f;
-      continue;
-    }
-    const float lp = a.logp[t], A = a.advantage[t];
-    const float r = expf(lp - a.old_logp[t]);
-    const float rc = fminf(fmaxf(r, 1.f - a.low), 1.f + a.high);
+  // first: the thread that keeps the sums
+  __device__ float coefficient(const Rows& a, const Policy& p, const RowIn& in, float lp, bool first) {
+    const float w = w0 * in.share;
+    if (bad) return NAN;
+    if (w == 0.f) return 0.f;
+    const float A = in.advantage, r = expf(lp - in.old);
+    const float rc = fminf(fmaxf(r, 1.f - p.low), 1.f + p.high);
     // the smaller product; an advantage of zero takes nothing of a ratio that overflowed
     const bool free = !(r * A > rc * A);
     const float f = A == 0.f && !isnan(r) ? 0.f : free ? -r * A : -rc * A;
-    float slope = free ? f : 0.f;
-    term += (double)w * f;
-    clipped += free ? 0.0 : (double)w;
-    if (a.ref_logp) {
-      const float away = a.ref_logp[t] - lp, ex = expf(away);
-      klsum += (double)w * (isinf(ex) ? ex : ex - away - 1.f);
-      if (a.kl != 0.f) slope += a.kl * (1.f - ex);
+    float slope = free ? f : 0.f, kl = 0.f;
+    if (p.ref_logp) {
+      const float away = in.ref - lp, ex = expf(away);
+      kl = isinf(ex) ? ex : ex - away - 1.f;
+      if (p.kl != 0.f) slope += p.kl * (1.f - ex);
     }
-    a.coef[t] = a.scale * w * slope;
+    if (first) {
+      sum[0].add(w * f);
+      sum[1].add(w * kl);
+      sum[2].add(free ? 0.f : w);
+    }
+    return in.y < a.V ? p.scale * w * slope : NAN;
   }
-  term = block_sum_f64(term, red);
-  klsum = block_sum_f64(klsum, red);
-  clipped = block_sum_f64(clipped, red);
-  if (threadIdx.x == 0) {
-    a.part[3 * blockIdx.x] = term;
-    a.part[3 * blockIdx.x + 1] = klsum;
-    a.part[3 * blockIdx.x + 2] = clipped;
-    if (bad) atomicOr(&a.head->bad, 1);
-    last = atomic_add_acq_rel(&a.head->ticket, 1) == (int)gridDim.x - 1;
+  // the sums of a CTA's groups and of all CTAs, in order, by the CTA that comes last
+  __device__ void finish(const Policy& p, Sum (*red)[3], int* last, bool keeps) {
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    if (lane == 0)
+      for (int j = 0; j < 3; ++j) red[warp][j] = keeps ? sum[j] : Sum();
+    __syncthreads();
+    if (warp) return;
+    if (lane < 3) {
+      Sum s;
+      for (int i = 0; i < (int)blockDim.x / 32; ++i) s.add(red[i][lane]);
+      p.part[3 * blockIdx.x + lane] = make_float2(s.s, s.e);
+    }
+    __syncwarp();
+    if (lane == 0) *last = atomic_add_acq_rel(&p.head->ticket, 1) == (int)gridDim.x - 1;
+    __syncwarp();
+    if (!*last) return;
+    Sum s[3];
+    for (int i = lane; i < (int)gridDim.x; i += 32)
+      for (int j = 0; j < 3; ++j) {
+        const float2 v = __ldcg(p.part + 3 * i + j);
+        Sum q;
+        q.s = v.x;
+        q.e = v.y;
+        s[j].add(q);
+      }
+    for (int j = 0; j < 3; ++j)
+      for (int o = 16; o > 0; o >>= 1) s[j].add(shuffle_down(s[j], o));
+    if (lane) return;
+    for (int j = 0; j < 3; ++j) p.terms[j] = bad ? NAN : s[j].value();
+    if (bad) {
+      *p.loss = NAN;
+    } else if (p.kl != 0.f && (!isfinite(s[0].s) || !isfinite(s[1].s))) {
+      *p.loss = p.scale * (s[0].s + p.kl * s[1].s);
+    } else {
+      const double kl = p.kl != 0.f ? (double)p.kl * ((double)s[1].s + s[1].e) : 0.0;
+      *p.loss = isfinite(s[0].s) ? (float)((double)p.scale * ((double)s[0].s + s[0].e + kl)) : p.scale * s[0].s;
+    }
   }
+};
+
+// What all threads of a row need for its gradient, from the warp that works
+// it out.
+enum { kFast = 0, kFill = 1, kExtremeSum = 2, kExtreme = 3 };   // kFill: the row is k throughout (0 or NaN)
+struct __align__(16) Published {
+  float M, scale, at_y, xy;
+  float m, l2, k;
+  int kind;
+};
+
+// Maximum and sum of a row: for the warps that work out its scalars (the row's own, or the CTA's first).
+template <int G>
+__device__ __forceinline__ Online gather(Online o, float c, Shared& sh, int& turn, int rank, int ranks) {
+  o = warp_merge(o, c);
+  if (G == 32) return o;
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  if (lane == 0) sh.part[0][warp] = make_float2(o.m, o.s);
   __syncthreads();
-  if (!last || threadIdx.x) return;
-  double s[3] = {0.0, 0.0, 0.0};
-  for (int i = 0; i < (int)gridDim.x; ++i)
-    for (int j = 0; j < 3; ++j) s[j] += __ldcg(a.part + 3 * i + j);
-  for (int j = 0; j < 3; ++j) a.terms[j] = bad ? NAN : (float)s[j];
-  *a.loss = bad ? NAN : (float)((double)a.scale * (s[0] + (a.kl != 0.f ? (double)a.kl * s[1] : 0.0)));
+  auto among = [&](const float2* from, int n) {
+    Online q;
+    if (lane < n) {
+      q.m = from[lane].x;
+      q.s = from[lane].y;
+      q.M = ref_of(q.m, c);
+    }
+    return warp_merge(q, c);
+  };
+  if (warp == 0) o = among(sh.part[0], G / 32);
+  if (ranks == 1) return o;
+  const int b = turn++ & 1;
+  if (threadIdx.x < ranks) {
+    uint32_t at;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(&sh.cta[b][rank])), "r"((uint32_t)threadIdx.x));
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(o.m), "f"(o.s) : "memory");
+  }
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (warp == 0) o = among(sh.cta[b], ranks);
+  return o;
+}
+
+// Every row once, held in shared memory from the pass that sums its
+// exponentials to the pass that writes its gradient, which also starts the
+// next row's copies piece by piece: the logits are read once, and reads and
+// writes of memory overlap.  The grid stays; a group takes every groups-th row.
+// The scalars of a row are the first warp's, as issue slots bound this kernel.
+template <typename E, int G, int NT>
+__global__ void __launch_bounds__(NT, 768 / NT) policy_held_kernel(Rows a, Policy p, int most) {
+  extern __shared__ __align__(16) unsigned char rows_smem[];
+  __shared__ Shared sh;
+  __shared__ Published pub;
+  __shared__ Sum red[(NT / 32)][3];
+  __shared__ int last;
+  constexpr bool kWarpRow = G == 32;
+  const int rank = kWarpRow ? 0 : cluster_rank(), ranks = kWarpRow ? 1 : cluster_ranks();
+  const int tid = threadIdx.x % G;
+  const bool scalars = kWarpRow || threadIdx.x < 32;      // this warp works out the row's scalars
+  const bool first = tid == 0 && rank == 0;
+  const int64_t groups = kWarpRow ? gridDim.x * (int64_t)(NT / 32) : gridDim.x / ranks;
+  int64_t t = kWarpRow ? blockIdx.x * (int64_t)(NT / 32) + threadIdx.x / 32 : blockIdx.x / ranks;
+  const uint32_t at = smem_u32(rows_smem) + (kWarpRow ? (threadIdx.x / 32) * most * G * 16 : 0);
+  int turn = 0;
+  PolicyState state;
+  const E* x = static_cast<const E*>(a.x) + t * a.ld;
+  E* g = static_cast<E*>(a.g) + t * a.ldg;
+  const int64_t x_step = groups * a.ld, g_step = groups * a.ldg;
+  auto target_of = [&](int64_t row) { return row < a.T ? a.y[row] : -1; };
+  int32_t y = target_of(t), y1 = target_of(t + groups);
+  Held<E> row{nullptr, Slice{0, 0, 0, 0}, 0.f, -1};
+  if (y >= 0) {
+    row = hold(x, slice_of(x, a.V, rank, ranks), tid);
+    copy_row<E, G>(row, at, tid, most);
+  }
+  state.weigh(p);
+  RowIn in{-1, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (scalars) in = row_in<E>(a, p, t, y);
+  for (; t < a.T; t += groups, x += x_step, g += g_step) {
+    const int32_t y2 = target_of(t + 2 * groups);
+    const bool copy = y1 >= 0;
+    RowIn in1 = in;
+    Held<E> next = row;
+    if (copy) {
+      if (scalars) in1 = row_in<E>(a, p, t + groups, y1);
+      next = hold(x + x_step, slice_of(x + x_step, a.V, rank, ranks), tid);
+    }
+    Published q;
+    q.kind = kFill;
+    q.k = state.bad ? NAN : 0.f;
+    if (y >= 0) {
+      Online o = gather<G>(held_stats<E, G>(row, at, tid, a.c, most), a.c, sh, turn, rank, ranks);
+      auto work_out = [&](float L, int kind) {
+        const float lp = target_logp(in.xy, make_float2(o.m, L), a);
+        const float coef = state.coefficient(a, p, in, lp, first);
+        const RowGrad r = row_grad(o.m, L, coef, a.inv_tau, a.c, y);
+        if (first) p.logp[t] = lp;
+        q.M = r.M; q.scale = r.scale; q.at_y = r.at_y; q.xy = in.xy;
+        q.m = r.m; q.l2 = r.l2;
+        q.kind = coef == 0.f || isnan(coef) ? kFill : kind;
+        q.k = q.kind == kFill ? coef : r.k;
+      };
+      auto publish = [&] {
+        if (kWarpRow) return;
+        if (threadIdx.x == 0) pub = q;
+        __syncthreads();
+        q = pub;
+      };
+      if (scalars) {
+        if (is_extreme(o.m, a.c)) q.m = o.m, q.kind = kExtremeSum;
+        else work_out(logf(o.s) - kLn2 * fmaf(o.m, a.c, -o.M), kFast);
+      }
+      publish();
+      if (q.kind == kExtremeSum) {
+        const float m = q.m;
+        Online e;
+        e.m = e.M = 0.f;
+        e.s = held_sum_extreme<E, G>(row, at, tid, m, a.c);
+        e = gather<G>(e, a.c, sh, turn, rank, ranks);
+        if (scalars) work_out(logf(e.s), kExtreme);
+        publish();
+      }
+    } else if (first) {
+      p.logp[t] = 0.f;
+    }
+    const RowGrad r{q.m, q.M, a.c, q.scale, q.at_y, y, q.kind == kExtreme, q.l2, q.k};
+    if (a.g && q.kind == kFast) {
+      held_grad<E, G>(row, g, at, tid, q.xy, r, most, copy, next);
+    } else {
+      if (a.g && q.kind == kExtreme) held_grad_extreme<E, G>(row, g, at, tid, r);
+      if (a.g && q.kind == kFill) {
+        const Slice s = slice_of(x, a.V, rank, ranks);
+        slice_fill<E, G>(g, s.first, s.last, tid, q.k);
+      }
+      if (copy) copy_row<E, G>(next, at, tid, most);
+    }
+    row = next;
+    in = in1;
+    y = y1;
+    y1 = y2;
+  }
+  state.finish(p, red, &last, first);
+}
+
+// The same with the second reading from memory (the L2 cache, mostly).
+constexpr int kLongThreads = 1024;
+template <typename E>
+__global__ void __launch_bounds__(kLongThreads, 1) policy_long_kernel(Rows a, Policy p) {
+  constexpr int G = kLongThreads;
+  __shared__ Shared sh;
+  __shared__ Published pub;
+  __shared__ Sum red[G / 32][3];
+  __shared__ int last;
+  const int rank = cluster_rank(), ranks = cluster_ranks();
+  const int tid = threadIdx.x;
+  const bool scalars = tid < 32, first = tid == 0 && rank == 0;
+  int turn = 0;
+  PolicyState state;
+  state.weigh(p);
+  const int64_t groups = gridDim.x / ranks;
+  for (int64_t t = blockIdx.x / ranks; t < a.T; t += groups) {
+    const int32_t y = a.y[t];
+    const E* x = static_cast<const E*>(a.x) + t * a.ld;
+    E* g = static_cast<E*>(a.g) + t * a.ldg;
+    const Slice s = slice_of(x, a.V, rank, ranks);
+    Published q;
+    q.kind = kFill;
+    q.k = state.bad ? NAN : 0.f;
+    if (y >= 0) {
+      RowIn in{-1, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (scalars) in = row_in<E>(a, p, t, y);
+      Online o = gather<G>(slice_stats<E, G, kUnroll>(x, s, tid, a.c), a.c, sh, turn, rank, ranks);
+      auto work_out = [&](float L, int kind) {
+        const float lp = target_logp(in.xy, make_float2(o.m, L), a);
+        const float coef = state.coefficient(a, p, in, lp, first);
+        const RowGrad r = row_grad(o.m, L, coef, a.inv_tau, a.c, y);
+        if (first) p.logp[t] = lp;
+        q.M = r.M; q.scale = r.scale; q.at_y = r.at_y; q.xy = in.xy;
+        q.m = r.m; q.l2 = r.l2;
+        q.kind = coef == 0.f || isnan(coef) ? kFill : kind;
+        q.k = q.kind == kFill ? coef : r.k;
+      };
+      auto publish = [&] {
+        if (threadIdx.x == 0) pub = q;
+        __syncthreads();
+        q = pub;
+      };
+      if (scalars) {
+        if (is_extreme(o.m, a.c)) q.m = o.m, q.kind = kExtremeSum;
+        else work_out(logf(o.s) - kLn2 * fmaf(o.m, a.c, -o.M), kFast);
+      }
+      publish();
+      if (q.kind == kExtremeSum) {
+        Online e;
+        e.m = e.M = 0.f;
+        for (int v = s.first + tid; v < s.last; v += G) e.s += exp2f((Elem<E>::get(x + v) - q.m) * a.c);
+        e = gather<G>(e, a.c, sh, turn, rank, ranks);
+        if (scalars) work_out(logf(e.s), kExtreme);
+        publish();
+      }
+    } else if (first) {
+      p.logp[t] = 0.f;
+    }
+    if (!a.g) continue;
+    const RowGrad r{q.m, q.M, a.c, q.scale, q.at_y, y, q.kind == kExtreme, q.l2, q.k};
+    if (q.kind == kFill) slice_fill<E, G>(g, s.first, s.last, tid, q.k);
+    else slice_grad<E, G, kUnroll>(x, g, s, tid, q.xy, r);
+  }
+  state.finish(p, red, &last, first);
 }
 
 // ---- host --------------------------------------------------------------------
@@ -388,7 +695,7 @@ int check_rows(const pgc_logits* z, bool grad_required) {
 
 Rows rows_of(const pgc_logits* z) {
   const float inv_tau = 1.f / z->temperature;
-  return Rows{z->x, z->grad, z->target, z->rows, z->classes, z->ld, z->grad_ld, inv_tau, inv_tau * kLog2e};
+  return Rows{z->x, z->grad, z->target, z->rows, z->ld, z->grad_ld, (int32_t)z->classes, inv_tau, inv_tau * kLog2e};
 }
 
 int sm_count() {
@@ -398,33 +705,37 @@ int sm_count() {
   return n;
 }
 
-// How a call's rows lie on the grid: a warp each (short rows), a CTA each, or
-// a cluster each (few long rows).
-constexpr int64_t kWarpRowBytes = 4096;
+// How the rows of a streaming pass lie on the grid: a warp each, a CTA each, or
+// a cluster each.  A warp takes a row up to 24 KB where there are rows for all
+// warps (bf16, 8192 classes, forward and gradient: 115 and 181 us for 800 and
+// 1200 MB, at the copy rate; 164 and 192 with CTAs; at 32 KB the gradient turns: 191
+// and 175), else one up to 4 KB.  Few long rows are split over a cluster while
+// the SMs hold more CTAs and a part stays above 4 KB.
+constexpr int64_t kWarpRowBytes = 4 * 1024, kWarpManyRowsBytes = 24 * 1024;
 struct Shape {
   bool warp;
   int ranks;
   unsigned grid;
 };
 Shape shape_of(const pgc_logits* z) {
-  const int64_t bytes = z->classes * (z->dtype == PGC_BF16 ? 2 : 4);
-  Shape s{bytes <= kWarpRowBytes, 1, 0};
+  const int64_t bytes = z->classes * (z->dtype == PGC_BF16 ? 2 : 4), sms = sm_count();
+  Shape s{bytes <= kWarpRowBytes || (bytes <= kWarpManyRowsBytes && z->rows >= 32 * sms), 1, 0};
   if (s.warp) {
     s.grid = (unsigned)((z->rows + kWarps - 1) / kWarps);
     return s;
   }
-  const int64_t sms = sm_count();
   while (s.ranks < kMaxCluster && z->rows * s.ranks * 2 <= 2 * sms && bytes / (s.ranks * 2) >= kWarpRowBytes) s.ranks *= 2;
   s.grid = (unsigned)(z->rows * s.ranks);
   return s;
 }
 
 template <typename... P, typename... A>
-cudaError_t launch(void (*kernel)(P...), unsigned grid, int ranks, bool pdl, cudaStream_t st, A... args) {
+cudaError_t launch(void (*kernel)(P...), unsigned grid, int threads, int ranks, bool pdl, size_t smem, cudaStream_t st, A... args) {
   cudaLaunchAttribute attr[2];
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cfg.attrs = attr;
   if (ranks > 1) {
@@ -447,7 +758,7 @@ cudaError_t launch_stats(const pgc_logits* z, float* logp, float2* stats, Head* 
   const bool half = z->dtype == PGC_BF16;
   return launch(half ? s.warp ? row_stats_kernel<__nv_bfloat16, 32> : row_stats_kernel<__nv_bfloat16, kThreads>
                      : s.warp ? row_stats_kernel<float, 32> : row_stats_kernel<float, kThreads>,
-                s.grid, s.ranks, false, st, rows_of(z), logp, stats, head);
+                s.grid, kThreads, s.ranks, false, 0, st, rows_of(z), logp, stats, head);
 }
 
 cudaError_t launch_grad(const pgc_logits* z, const float* coef, const float2* stats, const Head* head, cudaStream_t st) {
@@ -456,38 +767,95 @@ cudaError_t launch_grad(const pgc_logits* z, const float* coef, const float2* st
   const bool half = z->dtype == PGC_BF16;
   return launch(half ? s.warp ? row_grad_kernel<__nv_bfloat16, 32> : row_grad_kernel<__nv_bfloat16, kThreads>
                      : s.warp ? row_grad_kernel<float, 32> : row_grad_kernel<float, kThreads>,
-                s.grid, s.ranks, head != nullptr, st, rows_of(z), coef, stats, head);
+                s.grid, kThreads, s.ranks, head != nullptr, 0, st, rows_of(z), coef, stats, head);
 }
 
 constexpr int kMaxParts = 1024;       // CTAs of the kernels that leave partial sums
 
+// Policy loss.  Rows up to 12 KB are a warp's (bf16, 4096 classes: 84 us with
+// warps, 104 with CTAs; at 16 KB 117 against 110), longer ones a CTA's: of 128
+// threads up to 36 KB, of 256 up to 110, of 512 above (a thread then has about
+// 16 places, and the SM as many warps as its shared memory allows rows for:
+// 16384 classes 111 us with 128 threads, 121 with 256).  A row between 110 and 148 KB
+// leaves room for no second one on the SM, so two CTAs of a cluster share it
+// (65536 classes: 217 us, 252 by one CTA); more CTAs per row cost more than
+// they bring, as each waits for the others of its row (100003 classes: 230 us by
+// one CTA, 355 by three), but where rows are too few for the SMs they halve a
+// row's time.  Above 216 KB a row is read twice by 1024 threads (131072
+// classes: 282 us; 338 in two halves held by two SMs).
+constexpr int64_t kHeldWarpBytes = 12 * 1024, kHeld128Bytes = 36 * 1024, kHeld256Bytes = 110 * 1024,
+                  kHeldPairBytes = 148 * 1024, kHeldSmem = 216 * 1024;
+template <typename E>
+cudaError_t launch_policy(const pgc_logits* z, const Policy& p, cudaStream_t st) {
+  const int64_t sms = sm_count(), pieces = z->classes / Elem<E>::N, bytes = pieces * 16;
+  const bool warp = bytes <= kHeldWarpBytes;
+  int ranks = 1;
+  if (!warp) {
+    if (bytes > kHeld256Bytes && bytes <= kHeldPairBytes) ranks = 2;
+    while (ranks < kMaxCluster && z->rows * ranks * 2 <= sms && bytes / ranks > 16384) ranks *= 2;
+  }
+  const int64_t slice = (pieces + ranks - 1) / ranks;
+  const int threads = warp ? 256 : slice * 16 <= kHeld128Bytes ? 128 : slice * 16 <= kHeld256Bytes ? 256 : 512;
+  const int group = warp ? 32 : threads;
+  const int most = (int)std::max<int64_t>(((slice + group - 1) / group + 1) / 2 * 2, 2);
+  const int64_t smem = (int64_t)most * 16 * threads;
+  const int64_t units = warp ? (z->rows + threads / 32 - 1) / (threads / 32) : z->rows * ranks;
+  if (smem > kHeldSmem) {
+    const unsigned grid = (unsigned)std::max<int64_t>(std::min<int64_t>(units, sms / ranks * ranks), ranks);
+    return launch(policy_long_kernel<E>, grid, kLongThreads, ranks, true, 0, st, rows_of(z), p);
+  }
+  const auto kernel = warp ? policy_held_kernel<E, 32, 256>
+                      : threads == 128 ? policy_held_kernel<E, 128, 128>
+                      : threads == 256 ? policy_held_kernel<E, 256, 256> : policy_held_kernel<E, 512, 512>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  int64_t most_ctas = sms * std::max<int64_t>(1, std::min<int64_t>(768 / threads, (226 * 1024) / (smem + 2048)));
+  if (ranks > 1) {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)ranks;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ranks);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess && n > 0) most_ctas = (int64_t)n * ranks;
+  }
+  most_ctas = std::min<int64_t>(most_ctas, kMaxParts) / ranks * ranks;
+  return launch(kernel, (unsigned)std::max<int64_t>(std::min(units, most_ctas), ranks), threads, ranks, true, (size_t)smem, st,
+                rows_of(z), p, most);
+}
+
 // Layout of the workspace (bytes): head, counts [kMaxParts], partial sums
-// [max(3 kMaxParts, sequences)] of 8 bytes, stats [rows], logp [rows], coef [rows], share [rows].
+// [kMaxParts][3] of 8, the pairs' losses [sequences], stats [rows], logp [rows],
+// coef or share [rows].
 struct Work {
   Head* head;
   int32_t* count;
-  double* part;
+  float2* sums;
   float2* stats;
-  float *logp, *coef, *share;
+  float *pair_loss, *logp, *coef, *share;
 };
-constexpr int64_t kHeadBytes = 256, kCountBytes = kMaxParts * 4;
-int64_t part_bytes(int64_t sequences) { return 8 * std::max<int64_t>(3 * kMaxParts, sequences); }
+constexpr int64_t kHeadBytes = 256, kCountBytes = kMaxParts * 4, kSumBytes = kMaxParts * 24;
 int64_t work_bytes(int64_t rows, int64_t sequences) {
-  return kHeadBytes + kCountBytes + part_bytes(sequences) + rows * 20;
+  return kHeadBytes + kCountBytes + kSumBytes + rows * 16 + sequences * 4;
 }
-Work work_at(void* ws, int64_t rows, int64_t sequences) {
+Work work_at(void* ws, int64_t rows) {
   char* p = static_cast<char*>(ws);
   Work w;
   w.head = reinterpret_cast<Head*>(p);
   p += kHeadBytes;
   w.count = reinterpret_cast<int32_t*>(p);
   p += kCountBytes;
-  w.part = reinterpret_cast<double*>(p);
-  p += part_bytes(sequences);
+  w.sums = reinterpret_cast<float2*>(p);
+  p += kSumBytes;
   w.stats = reinterpret_cast<float2*>(p);
   w.logp = reinterpret_cast<float*>(p + 8 * rows);
-  w.coef = w.logp + rows;
-  w.share = w.coef + rows;
+  w.coef = w.share = w.logp + rows;
+  w.pair_loss = w.coef + rows;
   return w;
 }
 int check_work(const void* ws, int64_t bytes, int64_t rows, int64_t sequences) {
@@ -538,14 +906,14 @@ int pgc_preference_loss(const pgc_logits *z, int32_t kind, int64_t pairs, const 
   if ((uintptr_t)offsets % 4 || (uintptr_t)ref_logp % 4 || (uintptr_t)loss % 4 || (uintptr_t)logp % 4) return PGC_EINVAL;
   rc = check_work(workspace, workspace_bytes, z->rows, 2 * pairs);
   if (rc) return rc;
-  const Work w = work_at(workspace, z->rows, 2 * pairs);
+  const Work w = work_at(workspace, z->rows);
   const cudaStream_t st = (cudaStream_t)stream;
+  Pref a{kind, average, pairs, z->rows, offsets, z->target, ref_logp, w.logp, beta, margin, smoothing, scale,
+         w.coef, logp, w.pair_loss, loss, w.head};
   cudaError_t e = z->rows ? launch_stats(z, w.logp, w.stats, w.head, st)
                           : cudaMemsetAsync(w.head, 0, sizeof(Head), st);
   if (e != cudaSuccess) return report_cuda(e);
-  Pref a{kind, average, pairs, z->rows, offsets, z->target, ref_logp, w.logp, beta, margin, smoothing, scale,
-         w.coef, logp, w.part, loss, w.head};
-  e = launch(pair_kernel, (unsigned)std::max<int64_t>(pairs, 1), 1, true, st, a);
+  e = launch(pair_kernel, (unsigned)std::max<int64_t>(pairs, 1), kThreads, 1, true, 0, st, a);
   if (e == cudaSuccess && z->grad) e = launch_grad(z, w.coef, w.stats, w.head, st);
   return report_cuda(e);
 }
@@ -567,21 +935,16 @@ int pgc_policy_loss(const pgc_logits *z, int32_t reduction, int64_t sequences, c
     if ((uintptr_t)p % 4) return PGC_EINVAL;
   rc = check_work(workspace, workspace_bytes, z->rows, sequences);
   if (rc) return rc;
-  const Work w = work_at(workspace, z->rows, sequences);
+  const Work w = work_at(workspace, z->rows);
   const cudaStream_t st = (cudaStream_t)stream;
   Policy a{reduction, z->rows, sequences, offsets, z->target, old_logp, ref_logp, advantage, logp, clip_low, clip_high,
-           kl, scale, w.coef, w.count, 0, w.share, w.part, loss, terms, w.head};
+           kl, scale, w.count, 0, w.share, w.sums, loss, terms, w.head};
   const int64_t units = reduction == PGC_MEAN_SEQUENCES ? sequences : (z->rows + kThreads - 1) / kThreads;
   a.counts = (int)std::min<int64_t>(std::max<int64_t>(units, 1), 64);
   count_kernel<<<a.counts, kThreads, 0, st>>>(a);
   cudaError_t e = cudaGetLastError();
-  if (e == cudaSuccess) e = launch_stats(z, logp, w.stats, nullptr, st);
   if (e != cudaSuccess) return report_cuda(e);
-  const int grid = (int)std::min<int64_t>(std::max<int64_t>((z->rows + kThreads - 1) / kThreads, 1), kMaxParts);
-  policy_kernel<<<grid, kThreads, 0, st>>>(a);
-  e = cudaGetLastError();
-  if (e == cudaSuccess && z->grad) e = launch_grad(z, w.coef, w.stats, w.head, st);
-  return report_cuda(e);
+  return report_cuda(z->dtype == PGC_BF16 ? launch_policy<__nv_bfloat16>(z, a, st) : launch_policy<float>(z, a, st));
 }
 
 }  // extern "C"

@@ -256,6 +256,44 @@ def test_preference(cuda, losses, dtype, V, lens, kw, ref):
     assert alone["dlogits"] is None and torch.equal(alone["loss"], res["loss"]) and torch.equal(alone["logp"], res["logp"])
 
 
+@pytest.mark.parametrize("dtype,V,lens,kw", [
+    ("bfloat16", 32768, [200, 0, 1, 300, 0, 0, 150, 249, 17, 83], dict(smoothing=0.1)),      # several pairs at once in flight
+    ("float32", 9001, [700, 800], dict(kind="squared", average=True)),                        # one pair of unaligned rows
+    ("bfloat16", 20001, [1, 2] * 500, dict(kind="hinge", temperature=1.2)),                   # pairs of three rows
+    ("float32", 131072, [60, 70], dict(average=True))])
+def test_preference_of_many_logits(cuda, losses, dtype, V, lens, kw):
+    """Enough rows for several waves of CTAs."""
+    torch = cuda
+    first, behind = 3, 2
+    T = first + sum(lens) + behind
+    r, x, y = make(torch, getattr(torch, dtype), T, V, masked=range(3, T, 7))
+    off, off_d = offsets_of(torch, lens, first)
+    pairs = len(lens) // 2
+    logp, _ = losses.token_logprob(x, y, kw.get("temperature", 1.0))
+    lp = on_host(logp)
+    held = [max(int((y[a:b] >= 0).sum()), 1) if kw.get("average") else 1 for a, b in zip(off[:-1], off[1:])]
+    score = np.array([lp[a:b].sum() / n for a, b, n in zip(off[:-1], off[1:], held)]).reshape(pairs, 2)
+    ref_d = torch.from_numpy((score + r.standard_normal((pairs, 2))).astype(np.float32)).cuda()
+    res = losses.preference_loss(x, y, off_d, ref_d, **kw)
+    check_preference(torch, res, x, y, off, ref_d, kw)
+    assert (res["dlogits"][:first] == 0).all() and (res["dlogits"][T - behind:] == 0).all()
+    for _ in range(3):
+        again = losses.preference_loss(x, y, off_d, ref_d, **kw)
+        assert all(torch.equal(res[k], again[k]) for k in res)
+    alone = losses.preference_loss(x, y, off_d, ref_d, grad=False, **kw)
+    assert torch.equal(alone["loss"], res["loss"]) and torch.equal(alone["logp"], res["logp"])
+    y[T // 2] = V
+    bad = losses.preference_loss(x, y, off_d, ref_d, **kw)
+    assert bad["loss"].isnan() and bad["dlogits"][T // 2].isnan().all()
+    y[T // 2] = 0
+    off_d[1] = T + 1
+    bad = losses.preference_loss(x, y, off_d, ref_d, **kw)
+    assert bad["loss"].isnan() and bad["dlogits"].isnan().all() and bad["logp"][0].isnan().all()
+    off_d[1] = int(off[1])
+    inside = losses.preference_loss(x, y, off_d, ref_d, out=x, **kw)
+    assert inside["dlogits"] is x and x.isfinite().all()
+
+
 def check_policy(torch, res, x, y, old, adv, ref, kw, off=None):
     tau = kw.get("temperature", 1.0)
     okw = {("tau" if k == "temperature" else k): v for k, v in kw.items() if k != "offsets"}
