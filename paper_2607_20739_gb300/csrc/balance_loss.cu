@@ -14,16 +14,19 @@
 #include "dev_common.cuh"
 #include "pgc.h"
 #include "pgc_internal.h"
+#include "row_slice.cuh"
 
 namespace pgc {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxExperts = 1024, kMaxChoices = 64;
+constexpr int kMaxGrid = 1024;
 
 struct Head {
-  int32_t tokens;   // n
+  int32_t tokens;                 // n
   int32_t ticket;
+  int32_t counts[kMaxExperts];
 };
 
 struct Balance {
@@ -33,142 +36,372 @@ struct Balance {
   int32_t* choice;
   int32_t* counts;
   float* loss;
-  double* part;
+  Sum* part;                      // [grid]
   Head* head;
   int64_t T, ld, ldg;
   int E, k, given;
+  int wide_x, wide_g;             // rows of logits / gradients in whole 16-byte pieces
   float alpha;
 };
 
-__device__ __forceinline__ float to_float(float v) { return v; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ void put(float* p, float v) { *p = v; }
-__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+// A token belongs to L lanes, lane l of them has experts l R .. l R + R - 1 in
+// registers (-inf behind the last expert): as many tokens per warp as fit.
+template <typename X, int R>
+__device__ __forceinline__ void load_experts(const X* x, int l, int E, bool wide, float (&v)[R]) {
+  const int e0 = l * R;
+  if (wide) {
+    constexpr int N = Elem<X>::N;
+#pragma unroll
+    for (int q = 0; q < R / N; ++q) {
+      uint4 piece = no_piece(Elem<X>::kLowest);
+      if (e0 + q * N < E) piece = load16(reinterpret_cast<const uint4*>(x + e0) + q);
+      Pair f[N / 2];
+      Elem<X>::widen(piece, f);
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) split(f[i], v[q * N + 2 * i], v[q * N + 2 * i + 1]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < R; ++j) v[j] = e0 + j < E ? Elem<X>::get(x + e0 + j) : -INFINITY;
+  }
+}
+template <typename X, int R>
+__device__ __forceinline__ void store_experts(X* g, int l, int E, bool wide, const float (&v)[R]) {
+  const int e0 = l * R;
+  if (wide) {
+    constexpr int N = Elem<X>::N;
+#pragma unroll
+    for (int q = 0; q < R / N; ++q) {
+      Pair f[N / 2];
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) f[i] = pair(v[q * N + 2 * i], v[q * N + 2 * i + 1]);
+      if (e0 + q * N < E) store16(reinterpret_cast<uint4*>(g + e0) + q, Elem<X>::narrow(f));
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < R; ++j)
+      if (e0 + j < E) Elem<X>::put(g + e0 + j, v[j]);
+  }
+}
 
-// A warp per token.  Largest first, ties to the lowest expert; an expert of
-// logit -inf (or NaN) is never chosen, its place in the choice is -1.
-template <typename X>
+template <int L>
+__device__ __forceinline__ unsigned group_max(unsigned v) {
+  if (L == 32) return __reduce_max_sync(0xffffffffu, v);
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+template <int L>
+__device__ __forceinline__ float group_max(float v) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+template <int L>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// Order of floats as unsigned numbers; 0 for what is never chosen (-inf, NaN).
+__device__ __forceinline__ unsigned order_of(float f) {
+  const unsigned u = __float_as_uint(f + 0.f);      // -0 as 0
+  return f > -INFINITY ? u ^ ((unsigned)((int)u >> 31) | 0x80000000u) : 0u;
+}
+// The choice by definition: the largest logit behind the last one chosen, in the
+// order (value, expert), k times.  Choice i is lane i % L's, which writes and
+// counts it if out is given; returns the lane's last one.
+template <int L, int R>
+__device__ __noinline__ int choose_exact(const float (&v)[R], int l, int k, int32_t* out, int* count) {
+  unsigned last = 0xffffffffu;
+  int last_e = -1, held = -1;
+  for (int i = 0; i < k; ++i) {
+    unsigned best = 0;
+    int best_e = kMaxExperts;
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      const unsigned o = order_of(v[j]);
+      const int e = l * R + j;
+      if ((o < last || (o == last && e > last_e)) && o > best) {
+        best = o;
+        best_e = e;
+      }
+    }
+    for (int s = L / 2; s > 0; s >>= 1) {
+      const unsigned o = __shfl_xor_sync(0xffffffffu, best, s);
+      const int e = __shfl_xor_sync(0xffffffffu, best_e, s);
+      if (o > best || (o == best && e < best_e)) {
+        best = o;
+        best_e = e;
+      }
+    }
+    if (l == (i & (L - 1))) {
+      held = best ? best_e : -1;
+      if (out) {
+        out[i] = held;
+        if (best) atomicAdd(count + best_e, 1);
+      }
+    }
+    last = best;
+    last_e = best_e;
+  }
+  return held;
+}
+
+// The same from keys of 32 bits, for k <= L: each lane sorts its own and the
+// group takes the largest head k times; returns lane i's choice i.  A bf16
+// logit and its expert fit one key (16 bits each, the lower expert the larger
+// key).  A float keeps the upper bits of its order and its place in the lane;
+// where two of the chosen, or the last of them and the next, agree in these upper
+// bits, the definition decides.
+template <typename X, int L, int R>
+__device__ __forceinline__ int choose_keys(const float (&v)[R], int l, int k) {
+  constexpr bool kWhole = sizeof(X) == 2;
+  constexpr int kBits = R == 8 ? 3 : 4;
+  constexpr unsigned kPlace = (1u << kBits) - 1;
+  static_assert(R == 8 || R == 16, "places of a lane");
+  unsigned key[R];
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    const unsigned o = order_of(v[j]);
+    key[j] = kWhole ? (o & 0xffff0000u) | (0xffffu - (unsigned)(l * R + j)) : (o & ~kPlace) | (kPlace - (unsigned)j);
+    key[j] = o ? key[j] : 0u;
+  }
+  // Batcher's odd-even merge sort, largest first
+#pragma unroll
+  for (int p = 1; p < R; p *= 2)
+#pragma unroll
+    for (int q = p; q >= 1; q /= 2)
+#pragma unroll
+      for (int j = q % p; j + q < R; j += 2 * q)
+#pragma unroll
+        for (int i = 0; i < q; ++i)
+          if (i + j + q < R && (i + j) / (2 * p) == (i + j + q) / (2 * p)) {
+            const unsigned hi = max(key[i + j], key[i + j + q]);
+            key[i + j + q] = min(key[i + j], key[i + j + q]);
+            key[i + j] = hi;
+          }
+  unsigned last = 0;
+  int held = -1;
+  bool unsure = false;
+  for (int i = 0; i < k; ++i) {
+    const unsigned best = group_max<L>(key[0]);
+    const bool mine = key[0] == best;
+    int e;
+    if (kWhole) {
+      e = 0xffff - (int)(best & 0xffffu);
+    } else {
+      unsigned who = __ballot_sync(0xffffffffu, mine);
+      if (L < 32) who = who >> (threadIdx.x % 32 / L * L) & ((1u << (L % 32)) - 1u);
+      unsure |= best && ((who & (who - 1)) || best >> kBits == last >> kBits);
+      e = (__ffs(who) - 1) * R + (int)(kPlace - (best & kPlace));
+    }
+    last = best;
+    if (l == i) held = best ? e : -1;
+#pragma unroll
+    for (int j = 0; j < R - 1; ++j) key[j] = mine ? key[j + 1] : key[j];
+    key[R - 1] = mine ? 0u : key[R - 1];
+  }
+  if (!kWhole) {
+    const unsigned next = group_max<L>(key[0]);
+    unsure |= next && next >> kBits == last >> kBits;
+    if (__any_sync(0xffffffffu, unsure)) {
+      const int exact = choose_exact<L, R>(v, l, k, nullptr, nullptr);
+      if (unsure) held = exact;
+    }
+  }
+  return held;
+}
+
+// Choices and counts of the rows that this CTA takes (every `step`-th block of
+// rows from block `first`); counts and tokens are in shared memory.
+template <typename X, int L, int R>
+__device__ __forceinline__ void choose_rows(const Balance& a, int64_t first, int64_t step, int* count, int* tokens) {
+  constexpr int kRows = 32 / L;                     // tokens per warp
+  const int lane = threadIdx.x % 32, l = lane % L;
+  int n = 0;
+  for (int64_t t0 = (first * (blockDim.x / 32) + threadIdx.x / 32) * kRows; t0 < a.T; t0 += step * (blockDim.x / 32) * kRows) {
+    const int64_t t = t0 + lane / L;
+    const bool on = t < a.T && (!a.mask || a.mask[t]);
+    int32_t* out = a.choice + t * a.k;
+    n += on && l == 0;
+    if (a.given) {
+      if (on)
+        for (int j = l; j < a.k; j += L)
+          if (out[j] >= 0 && out[j] < a.E) atomicAdd(count + out[j], 1);
+      continue;
+    }
+    float v[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) v[j] = -INFINITY;
+    if (on) load_experts<X, R>(static_cast<const X*>(a.x) + t * a.ld, l, a.E, a.wide_x, v);
+    if constexpr (R <= 16) {
+      const int e = choose_keys<X, L, R>(v, l, a.k);
+      if (t < a.T && l < a.k) {
+        out[l] = e;
+        if (e >= 0) atomicAdd(count + e, 1);
+      }
+    } else {
+      choose_exact<L, R>(v, l, a.k, t < a.T ? out : nullptr, count);
+    }
+  }
+  n = __reduce_add_sync(0xffffffffu, n);
+  if (lane == 0 && n) atomicAdd(tokens, n);
+}
+
+// Gradients of the same rows and the CTA's part of the loss (in thread 0);
+// counts in shared memory.
+template <typename X, int L, int R>
+__device__ __forceinline__ Sum grad_rows(const Balance& a, int64_t first, int64_t step, const int* counts, float base, Sum* red) {
+  constexpr int kRows = 32 / L;
+  const int lane = threadIdx.x % 32, l = lane % L;
+  float w[R];                                       // base times the counts of this lane's experts
+#pragma unroll
+  for (int j = 0; j < R; ++j) w[j] = l * R + j < a.E ? base * (float)counts[l * R + j] : 0.f;
+  Sum sum;
+  for (int64_t t0 = (first * (blockDim.x / 32) + threadIdx.x / 32) * kRows; t0 < a.T; t0 += step * (blockDim.x / 32) * kRows) {
+    const int64_t t = t0 + lane / L;
+    const bool on = t < a.T && (!a.mask || a.mask[t]);
+    float v[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) v[j] = -INFINITY;
+    if (on) load_experts<X, R>(static_cast<const X*>(a.x) + t * a.ld, l, a.E, a.wide_x, v);
+    float m = v[0];
+#pragma unroll
+    for (int j = 1; j < R; ++j) m = fmaxf(m, v[j]);
+    m = group_max<L>(m);
+    if (m == -INFINITY) m = 0.f;     // no part taken, or no expert left: all zeros (a NaN stays)
+    float s = 0.f, dot = 0.f;
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      v[j] = ex2((v[j] - m) * kLog2e);
+      s += v[j];
+      dot = fmaf(v[j], w[j], dot);
+    }
+    s = group_sum<L>(s);
+    dot = group_sum<L>(dot);
+    const float r = s == 0.f ? 0.f : 1.f / s;
+    dot *= r;
+    if (l == 0 && on) sum.add(dot);
+    if (a.g && t < a.T) {
+#pragma unroll
+      for (int j = 0; j < R; ++j) v[j] = v[j] * r * (w[j] - dot);
+      store_experts<X, R>(static_cast<X*>(a.g) + t * a.ldg, l, a.E, a.wide_g, v);
+    }
+  }
+  return block_sum(sum, red);
+}
+
+// alpha E / (k n^2)
+__device__ __forceinline__ float weight_of(const Balance& a, int tokens) {
+  const float n = (float)max(tokens, 1);
+  return a.alpha * (float)a.E / (float)a.k / n / n;
+}
+
+template <typename X, int L, int R>
 __global__ void __launch_bounds__(kThreads) choose_kernel(Balance a) {
   __shared__ int count[kMaxExperts];
   __shared__ int tokens;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   for (int e = threadIdx.x; e < a.E; e += kThreads) count[e] = 0;
   if (threadIdx.x == 0) tokens = 0;
   __syncthreads();
-  const int lane = threadIdx.x % 32;
-  for (int64_t t = blockIdx.x * (int64_t)kWarps + threadIdx.x / 32; t < a.T; t += gridDim.x * (int64_t)kWarps) {
-    const bool on = !a.mask || a.mask[t];
-    int32_t* out = a.choice + t * a.k;
-    if (on && lane == 0) atomicAdd(&tokens, 1);
-    if (a.given) {
-      if (on)
-        for (int j = lane; j < a.k; j += 32)
-          if (out[j] >= 0 && out[j] < a.E) atomicAdd(&count[out[j]], 1);
-      continue;
-    }
-    if (!on) {
-      for (int j = lane; j < a.k; j += 32) out[j] = -1;
-      continue;
-    }
-    const X* x = static_cast<const X*>(a.x) + t * a.ld;
-    float last = INFINITY;
-    int last_e = -1;
-    for (int j = 0; j < a.k; ++j) {
-      // the largest behind (last, last_e) in the order of the choice
-      float best = -INFINITY;
-      int best_e = a.E;
-      for (int e = lane; e < a.E; e += 32) {
-        const float v = to_float(x[e]);
-        if ((v < last || (v == last && e > last_e)) && v > best) {
-          best = v;
-          best_e = e;
-        }
-      }
-      for (int o = 16; o > 0; o >>= 1) {
-        const float v = __shfl_xor_sync(0xffffffffu, best, o);
-        const int e = __shfl_xor_sync(0xffffffffu, best_e, o);
-        if (v > best || (v == best && e < best_e)) {
-          best = v;
-          best_e = e;
-        }
-      }
-      const bool found = best_e < a.E;
-      if (lane == 0) {
-        out[j] = found ? best_e : -1;
-        if (found) atomicAdd(&count[best_e], 1);
-      }
-      last = best;
-      last_e = best_e;
-    }
-  }
+  choose_rows<X, L, R>(a, blockIdx.x, gridDim.x, count, &tokens);
   __syncthreads();
   for (int e = threadIdx.x; e < a.E; e += kThreads)
-    if (count[e]) atomicAdd(a.counts + e, count[e]);
+    if (count[e]) atomicAdd(a.head->counts + e, count[e]);
   if (threadIdx.x == 0 && tokens) atomicAdd(&a.head->tokens, tokens);
 }
 
-template <typename X>
+template <typename X, int L, int R>
 __global__ void __launch_bounds__(kThreads) balance_grad_kernel(Balance a) {
-  __shared__ float w[kMaxExperts];
-  __shared__ double red[kWarps];
+  __shared__ int count[kMaxExperts];               // every CTA reads the counts once: they are a few lines of the L2 cache
+  __shared__ Sum red[32];
   __shared__ int last;
-  const double n = max(a.head->tokens, 1);
-  for (int e = threadIdx.x; e < a.E; e += kThreads)
-    w[e] = (float)((double)a.alpha * a.E * a.counts[e] / (a.k * n * n));
-  __syncthreads();
-  const int lane = threadIdx.x % 32;
-  double sum = 0.0;
-  for (int64_t t = blockIdx.x * (int64_t)kWarps + threadIdx.x / 32; t < a.T; t += gridDim.x * (int64_t)kWarps) {
-    X* g = static_cast<X*>(a.g) + t * a.ldg;
-    if (a.mask && !a.mask[t]) {
-      if (a.g)
-        for (int e = lane; e < a.E; e += 32) put(g + e, 0.f);
-      continue;
-    }
-    const X* x = static_cast<const X*>(a.x) + t * a.ld;
-    float m = -INFINITY;
-    for (int e = lane; e < a.E; e += 32) m = fmaxf(m, to_float(x[e]));
-    m = warp_max(m);
-    if (m == -INFINITY) {
-      bool nan = false;
-      for (int e = lane; e < a.E; e += 32) nan |= isnan(to_float(x[e]));
-      if (!__any_sync(0xffffffffu, nan)) {   // no expert left
-        if (a.g)
-          for (int e = lane; e < a.E; e += 32) put(g + e, 0.f);
-        continue;
-      }
-    }
-    float s = 0.f, dot = 0.f;
-    for (int e = lane; e < a.E; e += 32) {
-      const float p = expf(to_float(x[e]) - m);
-      s += p;
-      dot += p * w[e];
-    }
-    s = warp_sum(s);
-    dot = warp_sum(dot) / s;
-    sum += dot;
-    if (a.g)
-      for (int e = lane; e < a.E; e += 32) {
-        const float p = expf(to_float(x[e]) - m) / s;
-        put(g + e, p * (w[e] - dot));
-      }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  for (int e = threadIdx.x; e < a.E; e += kThreads) {
+    count[e] = __ldcg(a.head->counts + e);
+    if (blockIdx.x == 0) a.counts[e] = count[e];
   }
-  if (lane == 0) red[threadIdx.x / 32] = sum;
+  const float base = weight_of(a, __ldcg(&a.head->tokens));
   __syncthreads();
+  const Sum sum = grad_rows<X, L, R>(a, blockIdx.x, gridDim.x, count, base, red);
   if (threadIdx.x == 0) {
-    sum = 0.0;
-    for (int i = 0; i < kWarps; ++i) sum += red[i];
     a.part[blockIdx.x] = sum;
     last = atomic_add_acq_rel(&a.head->ticket, 1) == (int)gridDim.x - 1;
   }
   __syncthreads();
-  if (!last || threadIdx.x) return;
-  sum = 0.0;
-  for (int i = 0; i < (int)gridDim.x; ++i) sum += __ldcg(a.part + i);
-  *a.loss = (float)sum;
+  if (!last) return;
+  Sum all;
+  for (int i = threadIdx.x; i < (int)gridDim.x; i += kThreads) {
+    const float2 v = __ldcg(reinterpret_cast<const float2*>(a.part) + i);
+    Sum q;
+    q.s = v.x;
+    q.e = v.y;
+    all.add(q);
+  }
+  all = block_sum(all, red);
+  if (threadIdx.x == 0) *a.loss = all.value();
 }
 
-constexpr int kMaxGrid = 1024;
-constexpr int64_t kWorkBytes = 256 + kMaxGrid * 8;
+// One CTA for few tokens: no counts to clear in memory, and one launch.
+constexpr int kSmallThreads = 1024;
+template <typename X, int L, int R>
+__global__ void __launch_bounds__(kSmallThreads) balance_small_kernel(Balance a) {
+  __shared__ int count[kMaxExperts];
+  __shared__ Sum red[32];
+  __shared__ int tokens;
+  for (int e = threadIdx.x; e < a.E; e += kSmallThreads) count[e] = 0;
+  if (threadIdx.x == 0) tokens = 0;
+  __syncthreads();
+  choose_rows<X, L, R>(a, 0, 1, count, &tokens);
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.E; e += kSmallThreads) a.counts[e] = count[e];
+  const Sum sum = grad_rows<X, L, R>(a, 0, 1, count, weight_of(a, tokens), red);
+  if (threadIdx.x == 0) *a.loss = sum.value();
+}
+
+constexpr int64_t kWorkBytes = (sizeof(Head) + 255) / 256 * 256 + kMaxGrid * sizeof(Sum);
+
+template <typename X, int L, int R>
+cudaError_t launch_balance(Balance a, cudaStream_t st) {
+  constexpr int64_t kSmall = 16384;      // logits of a call for one CTA
+  if (a.T * a.E <= kSmall) {
+    balance_small_kernel<X, L, R><<<1, kSmallThreads, 0, st>>>(a);
+    return cudaGetLastError();
+  }
+  cudaError_t e = cudaMemsetAsync(a.head, 0, offsetof(Head, counts) + a.E * sizeof(int32_t), st);
+  if (e != cudaSuccess) return e;
+  constexpr int kRows = kWarps * 32 / L;
+  int dev = 0, sms = 148;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    sms = 148;
+  const unsigned grid = (unsigned)std::min<int64_t>(std::min<int64_t>((a.T + kRows - 1) / kRows, (int64_t)sms * 4), kMaxGrid);
+  choose_kernel<X, L, R><<<grid, kThreads, 0, st>>>(a);
+  e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = st;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, balance_grad_kernel<X, L, R>, a);
+}
+// The fewest lanes that hold a token's experts, 8 each, and its choices, one each.
+template <typename X>
+cudaError_t launch_balance(const Balance& a, cudaStream_t st) {
+  if (a.E <= 32 && a.k <= 4) return launch_balance<X, 4, 8>(a, st);
+  if (a.E <= 64 && a.k <= 8) return launch_balance<X, 8, 8>(a, st);
+  if (a.E <= 128 && a.k <= 16) return launch_balance<X, 16, 8>(a, st);
+  if (a.E <= 256 && a.k <= 32) return launch_balance<X, 32, 8>(a, st);
+  if (a.E <= 512 && a.k <= 32) return launch_balance<X, 32, 16>(a, st);
+  return launch_balance<X, 32, 32>(a, st);
+}
 
 }  // namespace
 }  // namespace pgc
@@ -198,23 +431,16 @@ int pgc_balance_loss(int32_t dtype, int64_t rows, int64_t experts, const void *l
     return PGC_EINVAL;
   if (experts > kMaxExperts || k > kMaxChoices) return PGC_ENOTSUP;
   if (workspace_bytes < kWorkBytes) return PGC_ESCRATCH;
-  const cudaStream_t st = (cudaStream_t)stream;
   Balance a;
   a.x = logits; a.g = grad; a.mask = mask; a.choice = choice; a.counts = counts; a.loss = loss;
   a.head = static_cast<Head*>(workspace);
-  a.part = reinterpret_cast<double*>(static_cast<char*>(workspace) + 256);
+  a.part = reinterpret_cast<Sum*>(static_cast<char*>(workspace) + kWorkBytes - kMaxGrid * sizeof(Sum));
   a.T = rows; a.ld = ld; a.ldg = grad_ld; a.E = (int)experts; a.k = k; a.given = given; a.alpha = alpha;
-  cudaError_t e = cudaMemsetAsync(a.head, 0, sizeof(Head), st);
-  if (e == cudaSuccess) e = cudaMemsetAsync(counts, 0, (size_t)experts * 4, st);
-  if (e != cudaSuccess) return report_cuda(e);
-  const unsigned grid = (unsigned)std::min<int64_t>(std::max<int64_t>((rows + kWarps - 1) / kWarps, 1), kMaxGrid);
-  if (dtype == PGC_BF16) choose_kernel<__nv_bfloat16><<<grid, kThreads, 0, st>>>(a);
-  else choose_kernel<float><<<grid, kThreads, 0, st>>>(a);
-  e = cudaGetLastError();
-  if (e != cudaSuccess) return report_cuda(e);
-  if (dtype == PGC_BF16) balance_grad_kernel<__nv_bfloat16><<<grid, kThreads, 0, st>>>(a);
-  else balance_grad_kernel<float><<<grid, kThreads, 0, st>>>(a);
-  return report_cuda(cudaGetLastError());
+  const int64_t n = 16 / (int64_t)size;
+  a.wide_x = (uintptr_t)logits % 16 == 0 && ld % n == 0 && experts % n == 0;
+  a.wide_g = (uintptr_t)grad % 16 == 0 && grad_ld % n == 0 && experts % n == 0;
+  const cudaStream_t st = (cudaStream_t)stream;
+  return report_cuda(dtype == PGC_BF16 ? launch_balance<__nv_bfloat16>(a, st) : launch_balance<float>(a, st));
 }
 
 }  // extern "C"

@@ -30,40 +30,6 @@ struct Rows {
   float inv_tau, c;                   // 1 / tau, log2(e) / tau
 };
 
-// A sum with its rounding errors kept beside it (two-sum): the double unit is
-// slow enough here to hold up a row.
-struct Sum {
-  float s = 0.f, e = 0.f;
-  __device__ void add(float v) {
-    const float t = s + v, b = t - s;
-    e += (s - (t - b)) + (v - b);
-    s = t;
-  }
-  __device__ void add(const Sum& o) {
-    add(o.s);
-    e += o.e;
-  }
-  // infinities leave no error behind
-  __device__ float value() const { return isfinite(s) ? s + e : s; }
-  __device__ double value_f64() const { return isfinite(s) ? (double)s + e : s; }
-};
-
-__device__ __forceinline__ Sum shuffle_down(const Sum& v, int o) {
-  Sum q;
-  q.s = __shfl_down_sync(0xffffffffu, v.s, o);
-  q.e = __shfl_down_sync(0xffffffffu, v.e, o);
-  return q;
-}
-// The block's sum, in thread 0.
-__device__ Sum block_sum(Sum v, Sum* red) {
-  for (int o = 16; o > 0; o >>= 1) v.add(shuffle_down(v, o));
-  __syncthreads();
-  if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = v;
-  __syncthreads();
-  if (threadIdx.x == 0)
-    for (int i = 1; i < (int)blockDim.x / 32; ++i) v.add(red[i]);
-  return v;
-}
 // The block's sum, in all threads.
 __device__ int block_sum(int v, int* red) {
   v = __reduce_add_sync(0xffffffffu, v);
@@ -391,17 +357,23 @@ struct PolicyState {
   bool bad = false;
   float w0 = 1.f;
 
-  __device__ void weigh(const Policy& p) {
+  // by the CTA's first warp, for all: the counts are a few lines that every CTA reads
+  __device__ void weigh(const Policy& p, int2& all) {
     wait_for_previous();
-    int n = 0;
-    for (int i = threadIdx.x % 32; i < p.counts; i += 32) {
-      const int q = p.count[i];
-      bad |= q < 0;
-      n += q;
+    if (threadIdx.x < 32) {
+      int n = 0;
+      for (int i = threadIdx.x; i < p.counts; i += 32) {
+        const int q = p.count[i];
+        bad |= q < 0;
+        n += q;
+      }
+      bad = __any_sync(0xffffffffu, bad);
+      n = __reduce_add_sync(0xffffffffu, n);
+      if (threadIdx.x == 0) all = make_int2(n, bad);
     }
-    bad = __any_sync(0xffffffffu, bad);
-    n = __reduce_add_sync(0xffffffffu, n);
-    if (p.reduction != PGC_SUM) w0 = 1.f / (float)max(n, 1);
+    __syncthreads();
+    bad = all.y != 0;
+    if (p.reduction != PGC_SUM) w0 = 1.f / (float)max(all.x, 1);
   }
   // first: the thread that keeps the sums
   __device__ float coefficient(const Rows& a, const Policy& p, const RowIn& in, float lp, bool first) {
@@ -518,6 +490,7 @@ __global__ void __launch_bounds__(NT, 768 / NT) policy_held_kernel(Rows a, Polic
   __shared__ Shared sh;
   __shared__ Published pub;
   __shared__ Sum red[(NT / 32)][3];
+  __shared__ int2 counted;
   __shared__ int last;
   constexpr bool kWarpRow = G == 32;
   const int rank = kWarpRow ? 0 : cluster_rank(), ranks = kWarpRow ? 1 : cluster_ranks();
@@ -539,7 +512,7 @@ __global__ void __launch_bounds__(NT, 768 / NT) policy_held_kernel(Rows a, Polic
     row = hold(x, slice_of(x, a.V, rank, ranks), tid);
     copy_row<E, G>(row, at, tid, most);
   }
-  state.weigh(p);
+  state.weigh(p, counted);
   RowIn in{-1, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (scalars) in = row_in<E>(a, p, t, y);
   for (; t < a.T; t += groups, x += x_step, g += g_step) {
@@ -616,13 +589,14 @@ __global__ void __launch_bounds__(kLongThreads, 1) policy_long_kernel(Rows a, Po
   __shared__ Shared sh;
   __shared__ Published pub;
   __shared__ Sum red[G / 32][3];
+  __shared__ int2 counted;
   __shared__ int last;
   const int rank = cluster_rank(), ranks = cluster_ranks();
   const int tid = threadIdx.x;
   const bool scalars = tid < 32, first = tid == 0 && rank == 0;
   int turn = 0;
   PolicyState state;
-  state.weigh(p);
+  state.weigh(p, counted);
   const int64_t groups = gridDim.x / ranks;
   for (int64_t t = blockIdx.x / ranks; t < a.T; t += groups) {
     const int32_t y = a.y[t];

@@ -24,6 +24,40 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+// A sum with its rounding errors kept beside it (two-sum): the double unit is
+// slow enough here to hold up a row.
+struct Sum {
+  float s = 0.f, e = 0.f;
+  __device__ void add(float v) {
+    const float t = s + v, b = t - s;
+    e += (s - (t - b)) + (v - b);
+    s = t;
+  }
+  __device__ void add(const Sum& o) {
+    add(o.s);
+    e += o.e;
+  }
+  // infinities leave no error behind
+  __device__ float value() const { return isfinite(s) ? s + e : s; }
+  __device__ double value_f64() const { return isfinite(s) ? (double)s + e : s; }
+};
+
+__device__ __forceinline__ Sum shuffle_down(const Sum& v, int o) {
+  Sum q;
+  q.s = __shfl_down_sync(0xffffffffu, v.s, o);
+  q.e = __shfl_down_sync(0xffffffffu, v.e, o);
+  return q;
+}
+// The block's sum, in thread 0.
+__device__ __forceinline__ Sum block_sum(Sum v, Sum* red) {
+  for (int o = 16; o > 0; o >>= 1) v.add(shuffle_down(v, o));
+  __syncthreads();
+  if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = v;
+  __syncthreads();
+  if (threadIdx.x == 0)
+    for (int i = 1; i < (int)blockDim.x / 32; ++i) v.add(red[i]);
+  return v;
+}
 // Two floats side by side: one instruction does both (add, multiply, FMA).
 using Pair = unsigned long long;
 __device__ __forceinline__ Pair pair(float lo, float hi) {
