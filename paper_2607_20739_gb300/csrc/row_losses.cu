@@ -7,7 +7,9 @@
 // p_v = exp((x_v - m) / tau - L).  Every loss here is a function of the rows'
 // logp, so its gradient is coef_t ([v = y] - p_v) / tau with coef_t = dloss/dlogp_t.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
+#include <initializer_list>
 
 #include "pgc.h"
 #include "pgc_internal.h"
@@ -145,12 +147,13 @@ __global__ void __launch_bounds__(kThreads) row_stats_kernel(Rows a, float* logp
   }
 }
 
+// A row, or one of its `parts`, per group: nothing is exchanged between them.
 template <typename E, int G>
-__global__ void __launch_bounds__(kThreads) row_grad_kernel(Rows a, const float* coef, const float2* stats,
+__global__ void __launch_bounds__(kThreads) row_grad_kernel(Rows a, int parts, const float* coef, const float2* stats,
                                                             const Head* head) {
-  const int rank = G == 32 ? 0 : cluster_rank(), ranks = G == 32 ? 1 : cluster_ranks();
+  const int rank = G == 32 ? 0 : blockIdx.x % parts, ranks = G == 32 ? 1 : parts;
   const int tid = threadIdx.x % G;
-  const int64_t t = G == 32 ? blockIdx.x * (int64_t)kWarps + threadIdx.x / 32 : blockIdx.x / ranks;
+  const int64_t t = G == 32 ? blockIdx.x * (int64_t)kWarps + threadIdx.x / 32 : blockIdx.x / parts;
   if (t >= a.T) return;
   const int32_t y = a.y[t];
   E* g = static_cast<E*>(a.g) + t * a.ldg;
@@ -203,47 +206,67 @@ __device__ float pref_loss(const Pref& a, float gap, float* slope) {
 }
 
 // A pair's scores, loss and coefficients from its rows' log probabilities:
-// the CTA's work, the results in thread 0.
+// the CTA's work, the results in thread 0.  No doubles: a few of them take
+// longer than the rest.
 struct PairWork {
-  Sum red[kMaxWarps];
-  int count[kMaxWarps];
+  Sum red[2][kWarps];
+  int count[2][kWarps];
 };
 __device__ float2 finish_pair(const Pref& a, int64_t i, const int32_t (&at)[3], PairWork& sh) {
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   Sum score[2];
-  int n[2];
+  int n[2] = {0, 0};
+  for (int64_t t = at[0] + (int64_t)threadIdx.x; t < at[2]; t += kThreads) {
+    const int j = t >= at[1];
+    const float lp = __ldcg(a.logp + t);
+    if (a.y[t] < 0) continue;
+    score[0].add(j ? 0.f : lp);
+    score[1].add(j ? lp : 0.f);
+    n[0] += !j;
+    n[1] += j;
+  }
   for (int j = 0; j < 2; ++j) {
-    Sum s;
-    int m = 0;
-    for (int64_t t = at[j] + (int64_t)threadIdx.x; t < at[j + 1]; t += blockDim.x)
-      if (a.y[t] >= 0) {
-        s.add(__ldcg(a.logp + t));
-        ++m;
-      }
-    n[j] = max(block_sum(m, sh.count), 1);
-    score[j] = block_sum(s, sh.red);
-  }
-  float2 coef = make_float2(0.f, 0.f);
-  if (threadIdx.x == 0) {
-    double v[2], gap;
-    for (int j = 0; j < 2; ++j) {
-      v[j] = score[j].value_f64() / (a.average ? n[j] : 1);
-      a.seq[2 * i + j] = (float)v[j];
+    for (int o = 16; o > 0; o >>= 1) score[j].add(shuffle_down(score[j], o));
+    n[j] = __reduce_add_sync(0xffffffffu, n[j]);
+    if (lane == 0) {
+      sh.red[j][warp] = score[j];
+      sh.count[j][warp] = n[j];
     }
-    gap = v[0] - v[1] - (double)a.margin / a.beta;
-    if (a.ref) gap -= (double)a.ref[2 * i] - (double)a.ref[2 * i + 1];
-    float slope;
-    a.pair_loss[i] = pref_loss(a, (float)gap, &slope);
-    slope = slope * a.scale / (float)a.pairs;
-    coef = make_float2(slope / (a.average ? n[0] : 1), -slope / (a.average ? n[1] : 1));
   }
-  return coef;
+  __syncthreads();
+  if (warp) return make_float2(0.f, 0.f);
+  float share[2];
+  Sum gap;
+  for (int j = 0; j < 2; ++j) {
+    score[j] = lane < kWarps ? sh.red[j][lane] : Sum();
+    n[j] = __reduce_add_sync(0xffffffffu, lane < kWarps ? sh.count[j][lane] : 0);
+    for (int o = kWarps / 2; o > 0; o >>= 1) score[j].add(shuffle_down(score[j], o));
+    share[j] = a.average ? 1.f / (float)max(n[j], 1) : 1.f;
+    if (a.average) {
+      score[j].s = score[j].value() / (float)max(n[j], 1);
+      score[j].e = 0.f;
+    }
+    if (lane == 0) a.seq[2 * i + j] = score[j].value();
+    gap.add(j ? -score[j].s : score[j].s);
+    gap.e += j ? -score[j].e : score[j].e;
+  }
+  if (a.ref) {
+    gap.add(-a.ref[2 * i]);
+    gap.add(a.ref[2 * i + 1]);
+  }
+  gap.add(-a.margin / a.beta);
+  float slope;
+  const float loss = pref_loss(a, gap.value(), &slope);
+  if (lane == 0) a.pair_loss[i] = loss;
+  slope = slope * a.scale / (float)a.pairs;
+  return make_float2(slope * share[0], -slope * share[1]);
 }
 // The mean of the pairs' losses.
 __device__ void finish_loss(const Pref& a, bool bad, PairWork& sh) {
   Sum s;
-  for (int64_t j = threadIdx.x; j < a.pairs; j += blockDim.x) s.add(__ldcg(a.pair_loss + j));
-  s = block_sum(s, sh.red);
-  if (threadIdx.x == 0) *a.loss = bad ? NAN : a.pairs ? (float)(s.value_f64() * a.scale / (double)a.pairs) : 0.f;
+  for (int64_t j = threadIdx.x; j < a.pairs; j += kThreads) s.add(__ldcg(a.pair_loss + j));
+  s = block_sum(s, sh.red[0]);
+  if (threadIdx.x == 0) *a.loss = bad ? NAN : a.pairs ? s.value() * a.scale / (float)a.pairs : 0.f;
 }
 
 __global__ void __launch_bounds__(kThreads) pair_kernel(Pref a) {
@@ -427,14 +450,11 @@ struct PolicyState {
       for (int o = 16; o > 0; o >>= 1) s[j].add(shuffle_down(s[j], o));
     if (lane) return;
     for (int j = 0; j < 3; ++j) p.terms[j] = bad ? NAN : s[j].value();
-    if (bad) {
-      *p.loss = NAN;
-    } else if (p.kl != 0.f && (!isfinite(s[0].s) || !isfinite(s[1].s))) {
-      *p.loss = p.scale * (s[0].s + p.kl * s[1].s);
-    } else {
-      const double kl = p.kl != 0.f ? (double)p.kl * ((double)s[1].s + s[1].e) : 0.0;
-      *p.loss = isfinite(s[0].s) ? (float)((double)p.scale * ((double)s[0].s + s[0].e + kl)) : p.scale * s[0].s;
+    if (p.kl != 0.f) {
+      s[0].add(p.kl * s[1].s);
+      s[0].e += p.kl * s[1].e;
     }
+    *p.loss = bad ? NAN : p.scale * s[0].value();
   }
 };
 
@@ -735,13 +755,19 @@ cudaError_t launch_stats(const pgc_logits* z, float* logp, float2* stats, Head* 
                 s.grid, kThreads, s.ranks, false, 0, st, rows_of(z), logp, stats, head);
 }
 
+// The gradient pass takes a row in parts of 32 to 64 KB: smaller grains level
+// the last wave (2000 x 50001 fp32: 115 us, 124 with whole rows; parts of 16 KB 127).
+constexpr int64_t kGradPartBytes = 32 * 1024;
 cudaError_t launch_grad(const pgc_logits* z, const float* coef, const float2* stats, const Head* head, cudaStream_t st) {
   if (z->rows == 0) return cudaSuccess;
   const Shape s = shape_of(z);
   const bool half = z->dtype == PGC_BF16;
+  const int64_t bytes = z->classes * (half ? 2 : 4), most = INT32_MAX / z->rows;
+  const int parts = s.warp ? 1 : (int)std::min(std::max<int64_t>(s.ranks, bytes / kGradPartBytes), most);
   return launch(half ? s.warp ? row_grad_kernel<__nv_bfloat16, 32> : row_grad_kernel<__nv_bfloat16, kThreads>
                      : s.warp ? row_grad_kernel<float, 32> : row_grad_kernel<float, kThreads>,
-                s.grid, kThreads, s.ranks, head != nullptr, 0, st, rows_of(z), coef, stats, head);
+                s.warp ? s.grid : (unsigned)(z->rows * parts), kThreads, 1, head != nullptr, 0, st, rows_of(z), parts,
+                coef, stats, head);
 }
 
 constexpr int kMaxParts = 1024;       // CTAs of the kernels that leave partial sums
@@ -759,6 +785,19 @@ constexpr int kMaxParts = 1024;       // CTAs of the kernels that leave partial 
 // classes: 282 us; 338 in two halves held by two SMs).
 constexpr int64_t kHeldWarpBytes = 12 * 1024, kHeld128Bytes = 36 * 1024, kHeld256Bytes = 110 * 1024,
                   kHeldPairBytes = 148 * 1024, kHeldSmem = 216 * 1024;
+// Shared memory above 48 KB is asked for once per device and kernel.
+cudaError_t allow_smem(const void* kernel, int which) {
+  static std::atomic<uint32_t> allowed[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  std::atomic<uint32_t>* seen = dev >= 0 && dev < 64 ? &allowed[dev] : nullptr;
+  if (seen && seen->load(std::memory_order_acquire) >> which & 1u) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kHeldSmem);
+  if (e == cudaSuccess && seen) seen->fetch_or(1u << which, std::memory_order_release);
+  return e;
+}
+
 template <typename E>
 cudaError_t launch_policy(const pgc_logits* z, const Policy& p, cudaStream_t st) {
   const int64_t sms = sm_count(), pieces = z->classes / Elem<E>::N, bytes = pieces * 16;
@@ -781,23 +820,10 @@ cudaError_t launch_policy(const pgc_logits* z, const Policy& p, cudaStream_t st)
   const auto kernel = warp ? policy_held_kernel<E, 32, 256>
                       : threads == 128 ? policy_held_kernel<E, 128, 128>
                       : threads == 256 ? policy_held_kernel<E, 256, 256> : policy_held_kernel<E, 512, 512>;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kernel),
+                                   (warp ? 0 : threads == 128 ? 1 : threads == 256 ? 2 : 3) + (Elem<E>::N == 8 ? 4 : 0));
   if (e != cudaSuccess) return e;
   int64_t most_ctas = sms * std::max<int64_t>(1, std::min<int64_t>(768 / threads, (226 * 1024) / (smem + 2048)));
-  if (ranks > 1) {
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = (unsigned)ranks;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)ranks);
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = (size_t)smem;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess && n > 0) most_ctas = (int64_t)n * ranks;
-  }
   most_ctas = std::min<int64_t>(most_ctas, kMaxParts) / ranks * ranks;
   return launch(kernel, (unsigned)std::max<int64_t>(std::min(units, most_ctas), ranks), threads, ranks, true, (size_t)smem, st,
                 rows_of(z), p, most);

@@ -39,7 +39,6 @@ struct Sum {
   }
   // infinities leave no error behind
   __device__ float value() const { return isfinite(s) ? s + e : s; }
-  __device__ double value_f64() const { return isfinite(s) ? (double)s + e : s; }
 };
 
 __device__ __forceinline__ Sum shuffle_down(const Sum& v, int o) {
@@ -48,16 +47,20 @@ __device__ __forceinline__ Sum shuffle_down(const Sum& v, int o) {
   q.e = __shfl_down_sync(0xffffffffu, v.e, o);
   return q;
 }
-// The block's sum, in thread 0.
+// The block's sum, in thread 0 (red: one per warp).
 __device__ __forceinline__ Sum block_sum(Sum v, Sum* red) {
+  const int lane = threadIdx.x % 32, warps = blockDim.x / 32;
   for (int o = 16; o > 0; o >>= 1) v.add(shuffle_down(v, o));
   __syncthreads();
-  if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = v;
+  if (lane == 0) red[threadIdx.x / 32] = v;
   __syncthreads();
-  if (threadIdx.x == 0)
-    for (int i = 1; i < (int)blockDim.x / 32; ++i) v.add(red[i]);
+  if (threadIdx.x < 32) {
+    v = lane < warps ? red[lane] : Sum();
+    for (int o = 16; o > 0; o >>= 1) v.add(shuffle_down(v, o));
+  }
   return v;
 }
+
 // Two floats side by side: one instruction does both (add, multiply, FMA).
 using Pair = unsigned long long;
 __device__ __forceinline__ Pair pair(float lo, float hi) {
