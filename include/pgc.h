@@ -403,8 +403,8 @@ int pgc_gradient_noalloc(int32_t loss, int32_t dtype, int64_t m, int64_t d, cons
  *  - workspace: 16-byte aligned device memory of the bytes that
  *    pgc_loss_workspace / pgc_balance_workspace return; its contents do not
  *    matter before a call and mean nothing after it.
- *  - Sums, maxima and probabilities are held in 32 bits (sums over tokens in 64), a bf16
- *    gradient is rounded once.  A call repeated on the same inputs gives the same bits.
+ *  - Sums, maxima and probabilities are held in 32 bits (sums over tokens in two
+ *    floats), a bf16 gradient is rounded once.  A call repeated on the same inputs gives the same bits.
  *  - A row whose target is negative takes no part (prompts, padding): its logits are
  *    not read, its log probability is 0 and its gradient row is zeros.  A
  *    target >= classes is not followed: log probability, gradient row and

@@ -102,12 +102,15 @@ __device__ __forceinline__ Online merge(Online o, float c, Shared& sh, int& turn
   return warp_merge(q, c);
 }
 
+// Logarithm of a row's sum at its maximum.
+__device__ __forceinline__ float log_sum(const Online& o, float c) { return logf(o.s) - kLn2 * fmaf(o.m, c, -o.M); }
+
 // The row's largest logit and log sum, for all threads of the group.
 template <typename E, int G>
 __device__ __forceinline__ float2 row_stats(const E* x, const Slice& s, int tid, float c, Shared& sh, int& turn,
                                             int rank, int ranks) {
   Online o = merge<G>(slice_stats<E, G, kUnroll>(x, s, tid, c), c, sh, turn, rank, ranks);
-  if (!is_extreme(o.m, c)) return make_float2(o.m, logf(o.s) - kLn2 * fmaf(o.m, c, -o.M));
+  if (!is_extreme(o.m, c)) return make_float2(o.m, log_sum(o, c));
   Online q;
   q.M = 0.f;
   for (int v = s.first + tid; v < s.last; v += G) q.s += exp2f((Elem<E>::get(x + v) - o.m) * c);
@@ -187,22 +190,31 @@ struct Pref {
   Head* head;
 };
 
-// Loss of one pair's gap of log ratios, and its derivative.
+// Loss of one pair's gap of log ratios, and its derivative.  A branch of
+// weight 0 takes no part, so that an infinite gap (an answer that the model
+// cannot give) has the loss and slope of its limit.
 __device__ float pref_loss(const Pref& a, float gap, float* slope) {
   const float beta = a.beta, e = a.smoothing;
   const float h = beta * gap;
+  auto both = [e](float chosen, float rejected) {      // (1 - e) chosen + e rejected
+    return (e < 1.f ? (1.f - e) * chosen : 0.f) + (e > 0.f ? e * rejected : 0.f);
+  };
+  if (isnan(h)) {
+    *slope = h;
+    return h;
+  }
   if (a.kind == PGC_PREF_SIGMOID) {
     const float soft = log1pf(expf(-fabsf(h)));
     *slope = beta * (1.f / (1.f + expf(-h)) - (1.f - e));
-    return (1.f - e) * (soft + (isnan(h) ? h : fmaxf(-h, 0.f))) + e * (soft + fmaxf(h, 0.f));
+    return both(soft + fmaxf(-h, 0.f), soft + fmaxf(h, 0.f));
   }
   if (a.kind == PGC_PREF_HINGE) {
-    *slope = beta * ((h > -1.f ? e : 0.f) - (h < 1.f ? 1.f - e : 0.f)) + (isnan(h) ? h : 0.f);
-    return (1.f - e) * fmaxf(1.f - h, 0.f) + e * fmaxf(1.f + h, 0.f) + (isnan(h) ? h : 0.f);
+    *slope = beta * ((h > -1.f ? e : 0.f) - (h < 1.f ? 1.f - e : 0.f));
+    return both(fmaxf(1.f - h, 0.f), fmaxf(1.f + h, 0.f));
   }
   const float up = gap - 0.5f / beta, down = gap + 0.5f / beta;
-  *slope = 2.f * ((1.f - e) * up + e * down);
-  return (1.f - e) * up * up + e * down * down;
+  *slope = 2.f * both(up, down);
+  return both(up * up, down * down);
 }
 
 // A pair's scores, loss and coefficients from its rows' log probabilities:
@@ -466,7 +478,16 @@ struct __align__(16) Published {
   float m, l2, k;
   int kind;
 };
-
+// of a row with maximum m and log sum L; `first` writes its log probability and keeps its part of the sums
+__device__ __forceinline__ Published work_out(const Rows& a, const Policy& p, PolicyState& state, const RowIn& in, float m,
+                                              float L, int kind, int64_t t, bool first) {
+  const float lp = target_logp(in.xy, make_float2(m, L), a);
+  const float coef = state.coefficient(a, p, in, lp, first);
+  const RowGrad r = row_grad(m, L, coef, a.inv_tau, a.c, in.y);
+  if (first) p.logp[t] = lp;
+  const bool fill = coef == 0.f || isnan(coef);
+  return Published{r.M, r.scale, r.at_y, in.xy, r.m, r.l2, fill ? coef : r.k, fill ? kFill : kind};
+}
 // Maximum and sum of a row: for the warps that work out its scalars (the row's own, or the CTA's first).
 template <int G>
 __device__ __forceinline__ Online gather(Online o, float c, Shared& sh, int& turn, int rank, int ranks) {
@@ -503,7 +524,8 @@ __device__ __forceinline__ Online gather(Online o, float c, Shared& sh, int& tur
 // exponentials to the pass that writes its gradient, which also starts the
 // next row's copies piece by piece: the logits are read once, and reads and
 // writes of memory overlap.  The grid stays; a group takes every groups-th row.
-// The scalars of a row are the first warp's, as issue slots bound this kernel.
+// The scalars of a row are the first warp's: eight warps working them out cost
+// a tenth of the kernel's time in issue slots.
 template <typename E, int G, int NT>
 __global__ void __launch_bounds__(NT, 768 / NT) policy_held_kernel(Rows a, Policy p, int most) {
   extern __shared__ __align__(16) unsigned char rows_smem[];
@@ -549,16 +571,6 @@ __global__ void __launch_bounds__(NT, 768 / NT) policy_held_kernel(Rows a, Polic
     q.k = state.bad ? NAN : 0.f;
     if (y >= 0) {
       Online o = gather<G>(held_stats<E, G>(row, at, tid, a.c, most), a.c, sh, turn, rank, ranks);
-      auto work_out = [&](float L, int kind) {
-        const float lp = target_logp(in.xy, make_float2(o.m, L), a);
-        const float coef = state.coefficient(a, p, in, lp, first);
-        const RowGrad r = row_grad(o.m, L, coef, a.inv_tau, a.c, y);
-        if (first) p.logp[t] = lp;
-        q.M = r.M; q.scale = r.scale; q.at_y = r.at_y; q.xy = in.xy;
-        q.m = r.m; q.l2 = r.l2;
-        q.kind = coef == 0.f || isnan(coef) ? kFill : kind;
-        q.k = q.kind == kFill ? coef : r.k;
-      };
       auto publish = [&] {
         if (kWarpRow) return;
         if (threadIdx.x == 0) pub = q;
@@ -567,7 +579,7 @@ __global__ void __launch_bounds__(NT, 768 / NT) policy_held_kernel(Rows a, Polic
       };
       if (scalars) {
         if (is_extreme(o.m, a.c)) q.m = o.m, q.kind = kExtremeSum;
-        else work_out(logf(o.s) - kLn2 * fmaf(o.m, a.c, -o.M), kFast);
+        else q = work_out(a, p, state, in, o.m, log_sum(o, a.c), kFast, t, first);
       }
       publish();
       if (q.kind == kExtremeSum) {
@@ -576,7 +588,7 @@ __global__ void __launch_bounds__(NT, 768 / NT) policy_held_kernel(Rows a, Polic
         e.m = e.M = 0.f;
         e.s = held_sum_extreme<E, G>(row, at, tid, m, a.c);
         e = gather<G>(e, a.c, sh, turn, rank, ranks);
-        if (scalars) work_out(logf(e.s), kExtreme);
+        if (scalars) q = work_out(a, p, state, in, o.m, logf(e.s), kExtreme, t, first);
         publish();
       }
     } else if (first) {
@@ -630,16 +642,6 @@ __global__ void __launch_bounds__(kLongThreads, 1) policy_long_kernel(Rows a, Po
       RowIn in{-1, 0.f, 0.f, 0.f, 0.f, 0.f};
       if (scalars) in = row_in<E>(a, p, t, y);
       Online o = gather<G>(slice_stats<E, G, kUnroll>(x, s, tid, a.c), a.c, sh, turn, rank, ranks);
-      auto work_out = [&](float L, int kind) {
-        const float lp = target_logp(in.xy, make_float2(o.m, L), a);
-        const float coef = state.coefficient(a, p, in, lp, first);
-        const RowGrad r = row_grad(o.m, L, coef, a.inv_tau, a.c, y);
-        if (first) p.logp[t] = lp;
-        q.M = r.M; q.scale = r.scale; q.at_y = r.at_y; q.xy = in.xy;
-        q.m = r.m; q.l2 = r.l2;
-        q.kind = coef == 0.f || isnan(coef) ? kFill : kind;
-        q.k = q.kind == kFill ? coef : r.k;
-      };
       auto publish = [&] {
         if (threadIdx.x == 0) pub = q;
         __syncthreads();
@@ -647,7 +649,7 @@ __global__ void __launch_bounds__(kLongThreads, 1) policy_long_kernel(Rows a, Po
       };
       if (scalars) {
         if (is_extreme(o.m, a.c)) q.m = o.m, q.kind = kExtremeSum;
-        else work_out(logf(o.s) - kLn2 * fmaf(o.m, a.c, -o.M), kFast);
+        else q = work_out(a, p, state, in, o.m, log_sum(o, a.c), kFast, t, first);
       }
       publish();
       if (q.kind == kExtremeSum) {
@@ -655,7 +657,7 @@ __global__ void __launch_bounds__(kLongThreads, 1) policy_long_kernel(Rows a, Po
         e.m = e.M = 0.f;
         for (int v = s.first + tid; v < s.last; v += G) e.s += exp2f((Elem<E>::get(x + v) - q.m) * a.c);
         e = gather<G>(e, a.c, sh, turn, rank, ranks);
-        if (scalars) work_out(logf(e.s), kExtreme);
+        if (scalars) q = work_out(a, p, state, in, o.m, logf(e.s), kExtreme, t, first);
         publish();
       }
     } else if (first) {

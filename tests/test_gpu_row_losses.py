@@ -294,6 +294,24 @@ def test_preference_of_many_logits(cuda, losses, dtype, V, lens, kw):
     assert inside["dlogits"] is x and x.isfinite().all()
 
 
+def test_preference_of_impossible_answers(cuda, losses):
+    """An answer of probability 0: the limits of the losses."""
+    torch = cuda
+    _, x, y = make(torch, torch.float32, 4, 30)
+    off = torch.arange(5, dtype=torch.int32, device="cuda")
+    x[1, int(y[1])] = -float("inf")                 # the rejected answer of the first pair
+    for kind in ("sigmoid", "hinge"):
+        res = losses.preference_loss(x, y, off, kind=kind, beta=0.01)
+        rest = losses.preference_loss(x[2:], y[2:], off[:3], kind=kind, beta=0.01)
+        assert res["logp"][0, 1] == -float("inf") and (res["dlogits"][:2] == 0).all()
+        assert float(res["loss"]) == pytest.approx(float(rest["loss"]) / 2, rel=4 * U)
+        assert (res["dlogits"][2:] == rest["dlogits"] / 2).all()
+    assert losses.preference_loss(x, y, off, smoothing=0.1)["loss"] == float("inf")
+    assert losses.preference_loss(x, y, off, kind="squared")["loss"] == float("inf")
+    x[0, int(y[0])] = -float("inf")                 # and the chosen one
+    assert losses.preference_loss(x, y, off)["loss"].isnan()
+
+
 def check_policy(torch, res, x, y, old, adv, ref, kw, off=None):
     tau = kw.get("temperature", 1.0)
     okw = {("tau" if k == "temperature" else k): v for k, v in kw.items() if k != "offsets"}
