@@ -109,11 +109,14 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
-// Order of floats as unsigned numbers; 0 for what is never chosen (-inf, NaN).
+// Order of floats as unsigned numbers; below kChosen what is never chosen (-inf,
+// and NaN as -inf).
+constexpr unsigned kChosen = 0x00800000u;
 __device__ __forceinline__ unsigned order_of(float f) {
-  const unsigned u = __float_as_uint(f + 0.f);      // -0 as 0
-  return f > -INFINITY ? u ^ ((unsigned)((int)u >> 31) | 0x80000000u) : 0u;
+  const unsigned u = __float_as_uint(fmaxf(f, -INFINITY) + 0.f);      // -0 as 0
+  return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
 }
+
 // The choice by definition: the largest logit behind the last one chosen, in the
 // order (value, expert), k times.  Choice i is lane i % L's, which writes and
 // counts it if out is given; returns the lane's last one.
@@ -122,7 +125,7 @@ __device__ __noinline__ int choose_exact(const float (&v)[R], int l, int k, int3
   unsigned last = 0xffffffffu;
   int last_e = -1, held = -1;
   for (int i = 0; i < k; ++i) {
-    unsigned best = 0;
+    unsigned best = kChosen - 1;
     int best_e = kMaxExperts;
 #pragma unroll
     for (int j = 0; j < R; ++j) {
@@ -142,10 +145,10 @@ __device__ __noinline__ int choose_exact(const float (&v)[R], int l, int k, int3
       }
     }
     if (l == (i & (L - 1))) {
-      held = best ? best_e : -1;
+      held = best >= kChosen ? best_e : -1;
       if (out) {
         out[i] = held;
-        if (best) atomicAdd(count + best_e, 1);
+        if (held >= 0) atomicAdd(count + held, 1);
       }
     }
     last = best;
@@ -171,7 +174,6 @@ __device__ __forceinline__ int choose_keys(const float (&v)[R], int l, int k) {
   for (int j = 0; j < R; ++j) {
     const unsigned o = order_of(v[j]);
     key[j] = kWhole ? (o & 0xffff0000u) | (0xffffu - (unsigned)(l * R + j)) : (o & ~kPlace) | (kPlace - (unsigned)j);
-    key[j] = o ? key[j] : 0u;
   }
   // Batcher's odd-even merge sort, largest first
 #pragma unroll
@@ -190,7 +192,8 @@ __device__ __forceinline__ int choose_keys(const float (&v)[R], int l, int k) {
   unsigned last = 0;
   int held = -1;
   bool unsure = false;
-  for (int i = 0; i < k; ++i) {
+  // choice i; `left` of the lane's keys can still matter behind it
+  auto take = [&](int i, int left) {
     const unsigned best = group_max<L>(key[0]);
     const bool mine = key[0] == best;
     int e;
@@ -199,18 +202,25 @@ __device__ __forceinline__ int choose_keys(const float (&v)[R], int l, int k) {
     } else {
       unsigned who = __ballot_sync(0xffffffffu, mine);
       if (L < 32) who = who >> (threadIdx.x % 32 / L * L) & ((1u << (L % 32)) - 1u);
-      unsure |= best && ((who & (who - 1)) || best >> kBits == last >> kBits);
+      unsure |= best >= kChosen && ((who & (who - 1)) || best >> kBits == last >> kBits);
       e = (__ffs(who) - 1) * R + (int)(kPlace - (best & kPlace));
     }
     last = best;
-    if (l == i) held = best ? e : -1;
+    if (l == i) held = best >= kChosen ? e : -1;
 #pragma unroll
-    for (int j = 0; j < R - 1; ++j) key[j] = mine ? key[j + 1] : key[j];
-    key[R - 1] = mine ? 0u : key[R - 1];
+    for (int j = 0; j < R; ++j)
+      if (j < left) key[j] = mine ? (j + 1 < R ? key[j + 1] : 0u) : key[j];
+  };
+  if (R == 8 && k <= 8) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < k) take(i, 8 - i);
+  } else {
+    for (int i = 0; i < k; ++i) take(i, R);
   }
   if (!kWhole) {
     const unsigned next = group_max<L>(key[0]);
-    unsure |= next && next >> kBits == last >> kBits;
+    unsure |= next >= kChosen && next >> kBits == last >> kBits;
     if (__any_sync(0xffffffffu, unsure)) {
       const int exact = choose_exact<L, R>(v, l, k, nullptr, nullptr);
       if (unsure) held = exact;
