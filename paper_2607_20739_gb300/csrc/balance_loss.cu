@@ -45,8 +45,10 @@ struct Balance {
 };
 
 // What bounds it: instruction issue.  65536 tokens x 256 experts, k = 8, fp32:
-// 74 us, of which the choice 50 (480 instructions a token) and the gradient 27
-// (205); reading and writing the logits would take 20.  16384 x 128 bf16: 20 us on
+// 72 us, of which the choice 45 (its comparisons fill the ALU) and the gradient 27
+// (205 instructions a token); reading and writing the logits would take 20.  More or
+// fewer than 4 CTAs of 256 threads per SM are slower (67 us at 60000 x 256; 70 with 3, 72 to
+// 76 with 6 and 8).  16384 x 128 bf16: 18 us on
 // the GPU.
 //
 // A token belongs to L lanes, lane l of them has experts l R .. l R + R - 1 in
