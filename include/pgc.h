@@ -427,7 +427,7 @@ typedef struct pgc_logits {
   int64_t rows, classes;      /* 0 <= rows < 2^31, 1 <= classes < 2^31              */
   int64_t ld, grad_ld;        /* row pitches in elements, classes <= ld <= 2^31     */
   int32_t dtype;              /* PGC_F32 or PGC_BF16                                */
-  float   temperature;        /* tau > 0 (1: the logits as they are)                */
+  float   temperature;        /* tau > 0 (1: the logits as they are), log2(e) / tau finite */
 } pgc_logits;
 
 /* pgc_loss_workspace — bytes of workspace of a preference or policy loss over

@@ -678,7 +678,8 @@ int check_rows(const pgc_logits* z, bool grad_required) {
   if (!z) return PGC_EINVAL;
   if (z->dtype != PGC_F32 && z->dtype != PGC_BF16) return PGC_EINVAL;
   if (z->rows < 0 || z->rows > INT32_MAX || z->classes < 1 || z->classes > INT32_MAX) return PGC_EINVAL;
-  if (!(z->temperature > 0.f) || !std::isfinite(z->temperature) || !std::isfinite(1.f / z->temperature)) return PGC_EINVAL;
+  if (!(z->temperature > 0.f) || !std::isfinite(z->temperature)) return PGC_EINVAL;
+  if (!std::isfinite(1.f / z->temperature * kLog2e)) return PGC_EINVAL;
   const uintptr_t size = z->dtype == PGC_BF16 ? 2 : 4;
   const int64_t far = int64_t(1) << 31;
   if (z->ld < z->classes || z->ld > far) return PGC_EINVAL;

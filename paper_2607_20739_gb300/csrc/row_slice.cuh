@@ -7,8 +7,8 @@
 // does no harm, as any M close to it serves: its residue r = m c - M (exact,
 // one FMA) is taken out of the logarithm of the sum.  M is held above -1e38, so that a
 // thread that has met nothing but -inf (or the type's lowest value, as masks
-// write it) adds 0 instead of NaN; a whole row of such values, or one whose
-// products overflow, is `extreme` and goes through (x - m) c in place of it.
+// write it) adds 0 instead of NaN; a whole row of such values, or one of very
+// large products, is `extreme` and goes through (x - m) c in place of it.
 #pragma once
 
 #include "dev_common.cuh"
@@ -250,8 +250,9 @@ struct RowGrad {
   float l2;       // log2 of the sum at m (extreme rows)
   float k;        // -coef / tau (extreme rows)
 };
-// A row whose largest logit, or its product with c, leaves the range of the fast path.
-__device__ __forceinline__ bool is_extreme(float m, float c) { return !(fabsf(m) < 1e37f && fabsf(m * c) < 1e37f); }
+// A row whose largest logit leaves the range of the fast path: up to |m c| = 1e8
+// the residue m c - M is below 2^3, beyond it 2^residue would soon overflow.
+__device__ __forceinline__ bool is_extreme(float m, float c) { return !(fabsf(m) < 1e37f && fabsf(m * c) < 1e8f); }
 
 __device__ __forceinline__ RowGrad row_grad(float m, float L, float coef, float inv_tau, float c, int y) {
   RowGrad g;

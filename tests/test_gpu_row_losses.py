@@ -177,6 +177,26 @@ def test_masked_logits_and_values(cuda, losses):
         assert float(pol["loss"]) == pytest.approx(4.8, rel=16 * U)
 
 
+@pytest.mark.parametrize("tau", [1e-38, 1e-30, 1e30])
+def test_far_temperatures(cuda, losses, tau):
+    """So cold that one class is left, so hot that all are alike."""
+    torch = cuda
+    for V in (40, 7000):
+        _, x, y = make(torch, torch.float32, 3, V, seed=4)
+        top = x.argmax(1).to(torch.int32)
+        y[0] = top[0]
+        logp, stats = losses.token_logprob(x, y, tau)
+        one = torch.ones(3, device="cuda")
+        d = losses.token_logprob_grad(x, y, stats, one, tau)
+        pol = losses.policy_loss(x, y, logp.nan_to_num(neginf=0.0), -one, reduction="sum", temperature=tau)
+        assert torch.equal(pol["logp"], logp)
+        if tau > 1:
+            assert torch.allclose(logp, torch.full_like(logp, -float(np.log(V))), rtol=4 * U)
+        else:
+            assert logp[0] == 0 and (logp[1:] < -1e20).all()
+            assert (d[0] == 0).all()
+
+
 def offsets_of(torch, lens, first=0):
     off = np.concatenate([[first], first + np.cumsum(lens)]).astype(np.int32)
     return off, torch.from_numpy(off).cuda()

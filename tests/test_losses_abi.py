@@ -17,7 +17,7 @@ def logits(B, **kw):
 BAD_ROWS = [dict(x=None), dict(target=None), dict(rows=-1), dict(rows=1 << 31), dict(classes=0), dict(classes=1 << 31),
             dict(ld=9), dict(ld=(1 << 31) + 1), dict(dtype=2), dict(dtype=-1), dict(temperature=0.0),
             dict(temperature=-1.0), dict(temperature=float("nan")), dict(temperature=float("inf")),
-            dict(temperature=1e-45), dict(x=P + 1), dict(target=P + 2), dict(dtype=0, x=P + 2)]
+            dict(temperature=1e-45), dict(temperature=4e-39), dict(x=P + 1), dict(target=P + 2), dict(dtype=0, x=P + 2)]
 BAD_GRAD = [dict(grad_ld=9), dict(grad_ld=(1 << 31) + 1), dict(grad=P + 1), dict(grad=P, x=P, grad_ld=16),
             dict(dtype=0, grad=P + 2)]
 
