@@ -45,11 +45,10 @@ struct Balance {
 };
 
 // What bounds it: instruction issue.  65536 tokens x 256 experts, k = 8, fp32:
-// 72 us, of which the choice 45 (its comparisons fill the ALU) and the gradient 27
+// 64 us, of which the choice 37 (comparisons on the ALU) and the gradient 27
 // (205 instructions a token); reading and writing the logits would take 20.  More or
-// fewer than 4 CTAs of 256 threads per SM are slower (67 us at 60000 x 256; 70 with 3, 72 to
-// 76 with 6 and 8).  16384 x 128 bf16: 18 us on
-// the GPU.
+// fewer than 4 CTAs of 256 threads per SM are slower (with sorted keys 67 us at 60000 x 256; 70
+// with 3, 72 to 76 with 6 and 8).  16384 x 128 bf16: 18 us on the GPU.
 //
 // A token belongs to L lanes, lane l of them has experts l R .. l R + R - 1 in
 // registers (-inf behind the last expert): as many tokens per warp as fit.
@@ -231,10 +230,55 @@ __device__ __forceinline__ int choose_keys(const float (&v)[R], int l, int k) {
   return held;
 }
 
+// For a whole warp per token and k <= kFew: the k-th largest of the lanes'
+// maxima is no more than the k-th largest logit, and few logits reach it.  They are gathered, one
+// per lane, and the largest of them (ties: the lowest expert) is taken k times:
+// half the instructions of sorted lanes (60000 x 256 fp32, k = 8: 60 us for the call, 66
+// with sorted keys; 30000 x 384 bf16: 56, 60).  bf16 up to 256 experts stays with keys that
+// hold logit and expert at once (51, 56 this way).  -2: more than 32 reach it.
+constexpr int kFew = 8;
+template <int R>
+__device__ __forceinline__ int choose_few(const float (&v)[R], int lane, int k, uint2* slot) {
+  unsigned key[R], top = 0;
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    key[j] = order_of(v[j]);
+    top = max(top, key[j]);
+  }
+  unsigned least = 0;
+  for (int i = 0; i < k; ++i) {
+    least = __reduce_max_sync(0xffffffffu, top);
+    top = top == least ? 0u : top;
+  }
+  least = max(least, kChosen);
+  const unsigned below = (1u << lane) - 1u;
+  int n = 0;
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    const bool reaches = key[j] >= least;
+    const unsigned all = __ballot_sync(0xffffffffu, reaches);
+    const int at = n + __popc(all & below);
+    if (reaches && at < 32) slot[at] = make_uint2(key[j], (unsigned)(lane * R + j));
+    n += __popc(all);
+  }
+  __syncwarp();
+  uint2 mine = lane < n ? slot[lane] : make_uint2(0u, 0xffffffffu);
+  __syncwarp();
+  if (n > 32) return -2;
+  int held = -1;
+  for (int i = 0; i < k; ++i) {
+    const unsigned best = __reduce_max_sync(0xffffffffu, mine.x);
+    const unsigned e = __reduce_min_sync(0xffffffffu, mine.x == best ? mine.y : 0xffffffffu);
+    if (lane == i && best) held = (int)e;
+    if (mine.y == e) mine.x = 0u;
+  }
+  return held;
+}
+
 // Choices and counts of the rows that this CTA takes (every `step`-th block of
-// rows from block `first`); counts and tokens are in shared memory.
+// rows from block `first`); counts, tokens and slots (32 per warp) are in shared memory.
 template <typename X, int L, int R>
-__device__ __forceinline__ void choose_rows(const Balance& a, int64_t first, int64_t step, int* count, int* tokens) {
+__device__ __forceinline__ void choose_rows(const Balance& a, int64_t first, int64_t step, int* count, int* tokens, uint2* slots) {
   constexpr int kRows = 32 / L;                     // tokens per warp
   const int lane = threadIdx.x % 32, l = lane % L;
   int n = 0;
@@ -254,7 +298,13 @@ __device__ __forceinline__ void choose_rows(const Balance& a, int64_t first, int
     for (int j = 0; j < R; ++j) v[j] = -INFINITY;
     if (on) load_experts<X, R>(static_cast<const X*>(a.x) + t * a.ld, l, a.E, a.wide_x, v);
     if constexpr (R <= 16) {
-      const int e = choose_keys<X, L, R>(v, l, a.k);
+      int e = -2;
+      if constexpr (L == 32 && (sizeof(X) == 4 || R > 8)) {
+        if (a.k <= kFew) e = choose_few<R>(v, l, a.k, slots + (threadIdx.x / 32) * 32);
+        if (__any_sync(0xffffffffu, e == -2)) e = choose_keys<X, L, R>(v, l, a.k);
+      } else {
+        e = choose_keys<X, L, R>(v, l, a.k);
+      }
       if (t < a.T && l < a.k) {
         out[l] = e;
         if (e >= 0) atomicAdd(count + e, 1);
@@ -319,12 +369,13 @@ __device__ __forceinline__ float weight_of(const Balance& a, int tokens) {
 template <typename X, int L, int R>
 __global__ void __launch_bounds__(kThreads) choose_kernel(Balance a) {
   __shared__ int count[kMaxExperts];
+  __shared__ uint2 slots[L == 32 ? kThreads : 1];
   __shared__ int tokens;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   for (int e = threadIdx.x; e < a.E; e += kThreads) count[e] = 0;
   if (threadIdx.x == 0) tokens = 0;
   __syncthreads();
-  choose_rows<X, L, R>(a, blockIdx.x, gridDim.x, count, &tokens);
+  choose_rows<X, L, R>(a, blockIdx.x, gridDim.x, count, &tokens, slots);
   __syncthreads();
   for (int e = threadIdx.x; e < a.E; e += kThreads)
     if (count[e]) atomicAdd(a.head->counts + e, count[e]);
@@ -367,12 +418,13 @@ constexpr int kSmallThreads = 1024;
 template <typename X, int L, int R>
 __global__ void __launch_bounds__(kSmallThreads) balance_small_kernel(Balance a) {
   __shared__ int count[kMaxExperts];
+  __shared__ uint2 slots[L == 32 ? kSmallThreads : 1];
   __shared__ Sum red[32];
   __shared__ int tokens;
   for (int e = threadIdx.x; e < a.E; e += kSmallThreads) count[e] = 0;
   if (threadIdx.x == 0) tokens = 0;
   __syncthreads();
-  choose_rows<X, L, R>(a, 0, 1, count, &tokens);
+  choose_rows<X, L, R>(a, 0, 1, count, &tokens, slots);
   __syncthreads();
   for (int e = threadIdx.x; e < a.E; e += kSmallThreads) a.counts[e] = count[e];
   const Sum sum = grad_rows<X, L, R>(a, 0, 1, count, weight_of(a, tokens), red);

@@ -478,6 +478,31 @@ def check_balance(torch, res, xs, loss, counts, g, k, alpha, n):
     assert abs(float(res["loss"]) - loss) <= es.sum() + 2 * U * abs(loss)
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("E", [5, 16, 33, 64, 128, 200, 256, 300, 512, 700])
+def test_balance_choice_among_equals(cuda, losses, dtype, E):
+    """Few distinct logits, zeros of both signs, infinities, NaN: the order is (value, lowest expert)."""
+    torch = cuda
+    r = np.random.default_rng(E)
+    for k in (1, 2, 7, 8, 9, 33, 64):
+        if k > E:
+            continue
+        for levels in (1, 2, 40, 100000):
+            T = int(r.integers(1, 120))
+            x = (r.integers(0, levels, (T, E)) - levels // 2).astype(np.float32) * np.float32(1e-3)
+            for value, share in ((-np.inf, 0.1), (np.nan, 0.02), (-0.0, 0.02), (np.inf, 0.01)):
+                x[r.random((T, E)) < share] = value
+            x = torch.from_numpy(x).cuda().to(getattr(torch, dtype))
+            mask = (r.random(T) < 0.8).astype(np.uint8)
+            got = losses.balance_loss(x, k, mask=torch.from_numpy(mask).cuda(), grad=False)
+            key = np.nan_to_num(x.float().cpu().numpy(), nan=-np.inf, posinf=np.inf, neginf=-np.inf) + 0.0
+            order = np.argsort(-key, axis=1, kind="stable")[:, :k]
+            want = np.where(np.take_along_axis(key, order, 1) > -np.inf, order, -1)
+            want[mask == 0] = -1
+            assert (got["choice"].cpu().numpy() == want).all(), (k, levels)
+            assert (got["counts"].cpu().numpy() == np.bincount(want[want >= 0], minlength=E)).all()
+
+
 def test_balance_ties_masks_and_given_choices(cuda, losses):
     torch = cuda
     x = torch.zeros(6, 40, device="cuda")
