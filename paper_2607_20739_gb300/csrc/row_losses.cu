@@ -217,18 +217,19 @@ __device__ float pref_loss(const Pref& a, float gap, float* slope) {
   return both(up * up, down * down);
 }
 
-// A pair's scores, loss and coefficients from its rows' log probabilities:
-// the CTA's work, the results in thread 0.  No doubles: a few of them take
-// longer than the rest.
+// A pair's scores, loss and coefficients from its rows' log probabilities, by
+// a warp (G = 32) or the CTA; the results are in lane 0 of its first warp.  No
+// doubles: a few of them take longer than the rest.
 struct PairWork {
   Sum red[2][kWarps];
   int count[2][kWarps];
 };
-__device__ float2 finish_pair(const Pref& a, int64_t i, const int32_t (&at)[3], PairWork& sh) {
+template <int G>
+__device__ __forceinline__ float2 finish_pair(const Pref& a, int64_t i, const int32_t (&at)[3], PairWork& sh) {
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   Sum score[2];
   int n[2] = {0, 0};
-  for (int64_t t = at[0] + (int64_t)threadIdx.x; t < at[2]; t += kThreads) {
+  for (int64_t t = at[0] + (int64_t)(threadIdx.x % G); t < at[2]; t += G) {
     const int j = t >= at[1];
     const float lp = __ldcg(a.logp + t);
     if (a.y[t] < 0) continue;
@@ -240,19 +241,23 @@ __device__ float2 finish_pair(const Pref& a, int64_t i, const int32_t (&at)[3], 
   for (int j = 0; j < 2; ++j) {
     for (int o = 16; o > 0; o >>= 1) score[j].add(shuffle_down(score[j], o));
     n[j] = __reduce_add_sync(0xffffffffu, n[j]);
-    if (lane == 0) {
+    if (G > 32 && lane == 0) {
       sh.red[j][warp] = score[j];
       sh.count[j][warp] = n[j];
     }
   }
-  __syncthreads();
-  if (warp) return make_float2(0.f, 0.f);
+  if (G > 32) {
+    __syncthreads();
+    if (warp) return make_float2(0.f, 0.f);
+    for (int j = 0; j < 2; ++j) {
+      score[j] = lane < kWarps ? sh.red[j][lane] : Sum();
+      n[j] = __reduce_add_sync(0xffffffffu, lane < kWarps ? sh.count[j][lane] : 0);
+      for (int o = kWarps / 2; o > 0; o >>= 1) score[j].add(shuffle_down(score[j], o));
+    }
+  }
   float share[2];
   Sum gap;
   for (int j = 0; j < 2; ++j) {
-    score[j] = lane < kWarps ? sh.red[j][lane] : Sum();
-    n[j] = __reduce_add_sync(0xffffffffu, lane < kWarps ? sh.count[j][lane] : 0);
-    for (int o = kWarps / 2; o > 0; o >>= 1) score[j].add(shuffle_down(score[j], o));
     share[j] = a.average ? 1.f / (float)max(n[j], 1) : 1.f;
     if (a.average) {
       score[j].s = score[j].value() / (float)max(n[j], 1);
@@ -281,34 +286,42 @@ __device__ void finish_loss(const Pref& a, bool bad, PairWork& sh) {
   if (threadIdx.x == 0) *a.loss = bad ? NAN : a.pairs ? s.value() * a.scale / (float)a.pairs : 0.f;
 }
 
+template <int G>
 __global__ void __launch_bounds__(kThreads) pair_kernel(Pref a) {
   __shared__ PairWork sh;
-  __shared__ float2 coef;
+  __shared__ float2 shared_coef;
   __shared__ int last;
-  const int64_t i = blockIdx.x;
+  const int64_t i = G == 32 ? blockIdx.x * (int64_t)kWarps + threadIdx.x / 32 : blockIdx.x;
+  const int tid = threadIdx.x % G;
   let_next_start();
   wait_for_previous();
   if (i < a.pairs) {
     const int32_t at[3] = {a.off[2 * i], a.off[2 * i + 1], a.off[2 * i + 2]};
     const bool bad = at[0] < 0 || at[1] < at[0] || at[2] < at[1] || at[2] > a.T;
     if (bad) {
-      if (threadIdx.x == 0) {
+      if (tid == 0) {
         a.seq[2 * i] = a.seq[2 * i + 1] = NAN;
         atomicOr(&a.head->bad, 1);
       }
     } else {
-      const float2 c = finish_pair(a, i, at, sh);
-      if (threadIdx.x == 0) coef = c;
-      __syncthreads();
-      for (int64_t t = at[0] + (int64_t)threadIdx.x; t < at[2]; t += kThreads) a.coef[t] = t < at[1] ? coef.x : coef.y;
+      float2 coef = finish_pair<G>(a, i, at, sh);
+      if (G == 32) {
+        coef.x = __shfl_sync(0xffffffffu, coef.x, 0);
+        coef.y = __shfl_sync(0xffffffffu, coef.y, 0);
+      } else {
+        if (tid == 0) shared_coef = coef;
+        __syncthreads();
+        coef = shared_coef;
+      }
+      for (int64_t t = at[0] + (int64_t)tid; t < at[2]; t += G) a.coef[t] = t < at[1] ? coef.x : coef.y;
     }
   }
   // rows outside every sequence
-  if (i == 0) {
+  if (blockIdx.x == 0) {
     const int64_t end = a.pairs ? min((int64_t)max(a.off[0], 0), a.T) : a.T;
     for (int64_t t = threadIdx.x; t < end; t += kThreads) a.coef[t] = 0.f;
   }
-  if (a.pairs && i == a.pairs - 1)
+  if (a.pairs && blockIdx.x == gridDim.x - 1)
     for (int64_t t = max(a.off[2 * a.pairs], 0) + (int64_t)threadIdx.x; t < a.T; t += kThreads) a.coef[t] = 0.f;
   __syncthreads();
   if (threadIdx.x == 0) last = atomic_add_acq_rel(&a.head->ticket, 1) == (int)gridDim.x - 1;
@@ -342,17 +355,25 @@ __global__ void __launch_bounds__(kThreads) count_kernel(Policy a) {
   int total = 0;
   bool bad = false;
   if (a.reduction == PGC_MEAN_SEQUENCES) {
-    for (int64_t s = blockIdx.x; s < a.S; s += gridDim.x) {
+    // a CTA per sequence, or a warp each where there are more of them than CTAs
+    const bool warp = a.S > gridDim.x;
+    const int tid = warp ? threadIdx.x % 32 : threadIdx.x, step = warp ? 32 : kThreads;
+    const int64_t first = warp ? blockIdx.x * (int64_t)kWarps + threadIdx.x / 32 : blockIdx.x;
+    for (int64_t s = first; s < a.S; s += warp ? gridDim.x * (int64_t)kWarps : gridDim.x) {
       const int64_t lo = a.off[s], hi = a.off[s + 1];
       if (lo < 0 || hi < lo || hi > a.T) {
         bad = true;
         continue;
       }
       int n = 0;
-      for (int64_t t = lo + threadIdx.x; t < hi; t += kThreads) n += a.y[t] >= 0;
-      n = block_sum(n, red);
+      for (int64_t t = lo + tid; t < hi; t += step) n += a.y[t] >= 0;
+      n = warp ? __reduce_add_sync(0xffffffffu, n) : block_sum(n, red);
       total += n > 0;
-      for (int64_t t = lo + threadIdx.x; t < hi; t += kThreads) a.share[t] = 1.f / (float)max(n, 1);
+      for (int64_t t = lo + tid; t < hi; t += step) a.share[t] = 1.f / (float)max(n, 1);
+    }
+    if (warp) {
+      total = block_sum(tid == 0 ? total : 0, red);
+      bad = __syncthreads_or(bad);
     }
     if (blockIdx.x == 0) {
       const int64_t end = a.S ? min((int64_t)max(a.off[0], 0), a.T) : a.T;
@@ -916,7 +937,10 @@ int pgc_preference_loss(const pgc_logits *z, int32_t kind, int64_t pairs, const 
   cudaError_t e = z->rows ? launch_stats(z, w.logp, w.stats, w.head, st)
                           : cudaMemsetAsync(w.head, 0, sizeof(Head), st);
   if (e != cudaSuccess) return report_cuda(e);
-  e = launch(pair_kernel, (unsigned)std::max<int64_t>(pairs, 1), kThreads, 1, true, 0, st, a);
+  // a warp per pair while pairs are short (64 rows a sequence): tens of thousands of them are a few waves
+  const bool warp = z->rows <= 128 * pairs;
+  e = launch(warp ? pair_kernel<32> : pair_kernel<kThreads>,
+             (unsigned)std::max<int64_t>(warp ? (pairs + kWarps - 1) / kWarps : pairs, 1), kThreads, 1, true, 0, st, a);
   if (e == cudaSuccess && z->grad) e = launch_grad(z, w.coef, w.stats, w.head, st);
   return report_cuda(e);
 }
@@ -943,7 +967,7 @@ int pgc_policy_loss(const pgc_logits *z, int32_t reduction, int64_t sequences, c
   Policy a{reduction, z->rows, sequences, offsets, z->target, old_logp, ref_logp, advantage, logp, clip_low, clip_high,
            kl, scale, w.count, 0, w.share, w.sums, loss, terms, w.head};
   const int64_t units = reduction == PGC_MEAN_SEQUENCES ? sequences : (z->rows + kThreads - 1) / kThreads;
-  a.counts = (int)std::min<int64_t>(std::max<int64_t>(units, 1), 64);
+  a.counts = (int)std::min<int64_t>(std::max<int64_t>(units, 1), 128);
   count_kernel<<<a.counts, kThreads, 0, st>>>(a);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return report_cuda(e);

@@ -252,6 +252,8 @@ def check_preference(torch, res, x, y, off, ref, kw):
     (20003, [3, 2, 1, 4], dict(margin=0.2, scale=0.5)),
     (131072, [2, 1], dict(beta=0.7)),
     (300, [1] * 600, dict(kind="sigmoid", beta=1.0)),
+    (10, [1, 0, 2, 3] * 700, dict(average=True, smoothing=0.2)),
+    (10, [130, 127, 128, 129], dict(scale=2.0)),
     (64, [700, 900], dict(average=True))])
 @pytest.mark.parametrize("ref", [True, False])
 def test_preference(cuda, losses, dtype, V, lens, kw, ref):
@@ -379,6 +381,8 @@ def away(drift, clip):
     (2, [30, 2], dict(kl=0.1, reduction="sequences")),
     (10, [400, 13, 1], dict(kl=0.05, clip=(0.1, 0.3), scale=2.0)),
     (257, [3, 0, 60], dict(reduction="sum", temperature=0.5)),
+    (10, [1, 0, 2, 3] * 400, dict(kl=0.1, reduction="sequences")),
+    (10, [40] * 130, dict(reduction="sequences")),
     (4099, [3, 4], dict(kl=0.3, reduction="sequences", temperature=1.5)),
     (20003, [2, 0, 7], dict(kl=0.01)),
     (50001, [4, 1], dict(reduction="sequences")),
@@ -576,7 +580,8 @@ def test_targets_and_offsets_that_are_none(cuda, losses):
         off = torch.tensor([0, 2, 4], dtype=torch.int32, device="cuda")
         assert losses.preference_loss(x, y, off)["loss"].isnan()
         y[2] = 1
-        for bad in ([0, 3, 2], [-1, 3, 4], [0, 3, 7], [5, 3, 1], [0, -2, 4], [0, 1 << 30, 4]):
+        many = [0] * 200 + [3, 2] + [4] * 199
+        for bad in ([0, 3, 2], [-1, 3, 4], [0, 3, 7], [5, 3, 1], [0, -2, 4], [0, 1 << 30, 4], many):
             off = torch.tensor(bad, dtype=torch.int32, device="cuda")
             res = losses.preference_loss(x, y, off)
             assert res["loss"].isnan() and res["dlogits"].isnan().all(), bad
