@@ -173,6 +173,90 @@ __global__ void __launch_bounds__(kThreads) row_grad_kernel(Rows a, int parts, c
   slice_grad<E, G, kUnroll>(x, g, s, tid, Elem<E>::get(x + y), row_grad(st.x, st.y, k, a.inv_tau, a.c, y));
 }
 
+// ---- short rows ----------------------------------------------------------------
+// Rows of up to L R classes in the registers of L lanes, single elements, so
+// that a warp has 32 / L rows at once: what a row costs there is its own
+// instructions, not its bytes.  (x - m) c serves rows of any range.
+template <int L>
+__device__ __forceinline__ float group_max(float v) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+template <int L>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+// A row's elements l, l + L, ... and -inf behind them (throughout, if not taken).
+template <typename E, int L, int R>
+__device__ __forceinline__ void short_load(const E* x, int l, int V, bool taken, float (&v)[R]) {
+#pragma unroll
+  for (int j = 0; j < R; ++j) v[j] = taken && l + j * L < V ? Elem<E>::get(x + l + j * L) : -INFINITY;
+}
+// (m, sum) of a row, v becoming 2^((x - m) c).  All lanes of the warp take part.
+template <int L, int R>
+__device__ __forceinline__ float2 short_exps(float (&v)[R], bool taken, float c) {
+  float m = v[0], s = 0.f;
+#pragma unroll
+  for (int j = 1; j < R; ++j) m = fmaxf(m, v[j]);
+  m = group_max<L>(m);
+  if (!taken) m = 0.f;
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    v[j] = ex2((v[j] - m) * c);
+    s += v[j];
+  }
+  return make_float2(m, group_sum<L>(s));
+}
+// k ([v = y] - p) / tau of the row, where v times scale is p; 0 or NaN throughout with such a k.
+template <typename E, int L, int R>
+__device__ __forceinline__ void short_store(E* g, int l, int V, const float (&v)[R], float scale, float k, float inv_tau, int y) {
+  const bool fill = k == 0.f || isnan(k);
+  const float at = k * inv_tau;
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    const int e = l + j * L;
+    if (e < V) Elem<E>::put(g + e, fill ? k : fmaf(v[j] * scale, -at, e == y ? at : 0.f));
+  }
+}
+
+template <typename E, int L, int R>
+__global__ void __launch_bounds__(kThreads) short_stats_kernel(Rows a, float* logp, float2* stats, Head* head) {
+  const int lane = threadIdx.x % 32, l = lane % L;
+  const int64_t t = (blockIdx.x * (int64_t)kWarps + threadIdx.x / 32) * (32 / L) + lane / L;
+  let_next_start();
+  if (head && blockIdx.x == 0 && threadIdx.x == 0) *head = Head{0, 0};
+  const int32_t y = t < a.T ? a.y[t] : -1;
+  const E* x = static_cast<const E*>(a.x) + t * a.ld;
+  float v[R];
+  short_load<E, L>(x, l, a.V, y >= 0, v);
+  const float xy = y >= 0 ? y < a.V ? Elem<E>::get(x + y) : NAN : 0.f;
+  const float2 ms = short_exps<L>(v, y >= 0, a.c);
+  if (l || t >= a.T) return;
+  const float2 st = y >= 0 ? make_float2(ms.x, logf(ms.y)) : make_float2(0.f, 0.f);
+  logp[t] = y >= 0 ? target_logp(xy, st, a) : 0.f;
+  stats[t] = st;
+}
+
+template <typename E, int L, int R>
+__global__ void __launch_bounds__(kThreads) short_grad_kernel(Rows a, const float* coef, const float2* stats, const Head* head) {
+  const int lane = threadIdx.x % 32, l = lane % L;
+  const int64_t t = (blockIdx.x * (int64_t)kWarps + threadIdx.x / 32) * (32 / L) + lane / L;
+  if (t >= a.T) return;
+  const int32_t y = a.y[t];
+  float v[R];
+  short_load<E, L>(static_cast<const E*>(a.x) + t * a.ld, l, a.V, y >= 0, v);
+  if (head) wait_for_previous();
+  const bool bad = head && head->bad;
+  const float k = bad || y >= a.V ? NAN : y < 0 ? 0.f : coef[t];
+  const float2 st = y >= 0 ? stats[t] : make_float2(0.f, 0.f);
+#pragma unroll
+  for (int j = 0; j < R; ++j) v[j] = ex2((v[j] - st.x) * a.c - st.y * kLog2e);
+  short_store<E, L>(static_cast<E*>(a.g) + t * a.ldg, l, a.V, v, 1.f, k, a.inv_tau, y);
+}
+
 // ---- preference ------------------------------------------------------------
 
 struct Pref {
@@ -634,6 +718,39 @@ __global__ void __launch_bounds__(NT, 768 / NT) policy_held_kernel(Rows a, Polic
   state.finish(p, red, &last, first);
 }
 
+// Short rows: from and to memory through registers.
+template <typename E, int L, int R>
+__global__ void __launch_bounds__(kThreads, 4) policy_short_kernel(Rows a, Policy p) {
+  __shared__ Sum red[kWarps][3];
+  __shared__ int2 counted;
+  __shared__ int last;
+  constexpr int kRows = 32 / L;
+  const int lane = threadIdx.x % 32, l = lane % L;
+  PolicyState state;
+  state.weigh(p, counted);
+  for (int64_t t0 = (blockIdx.x * (int64_t)kWarps + threadIdx.x / 32) * kRows; t0 < a.T;
+       t0 += gridDim.x * (int64_t)kWarps * kRows) {
+    const int64_t t = t0 + lane / L;
+    const int32_t y = t < a.T ? a.y[t] : -1;
+    const RowIn in = row_in<E>(a, p, t, y);
+    float v[R];
+    short_load<E, L>(static_cast<const E*>(a.x) + t * a.ld, l, a.V, y >= 0, v);
+    const float2 ms = short_exps<L>(v, y >= 0, a.c);
+    if (t >= a.T) continue;
+    float coef = state.bad ? NAN : 0.f, lp = 0.f;
+    if (y >= 0) {
+      lp = target_logp(in.xy, make_float2(ms.x, logf(ms.y)), a);
+      coef = state.coefficient(a, p, in, lp, l == 0);
+    }
+    if (l == 0) p.logp[t] = lp;
+    if (a.g) short_store<E, L>(static_cast<E*>(a.g) + t * a.ldg, l, a.V, v, 1.f / ms.y, coef, a.inv_tau, y);
+  }
+  __syncwarp();
+  for (int j = 0; j < 3; ++j)
+    for (int o = 16; o >= L; o >>= 1) state.sum[j].add(shuffle_down(state.sum[j], o));
+  state.finish(p, red, &last, lane == 0);
+}
+
 // The same with the second reading from memory (the L2 cache, mostly).
 constexpr int kLongThreads = 1024;
 template <typename E>
@@ -770,8 +887,34 @@ cudaError_t launch(void (*kernel)(P...), unsigned grid, int threads, int ranks, 
   return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
 }
 
+// Short rows: up to 128 classes by 8 lanes, 256 by 16, fp32 up to 512 by 32; rows
+// above are read in 16-byte pieces by a warp.  131072 rows of 10, 100 and 256 bf16
+// classes: forward 15, 14 and 25 us a call (36, 46 and 50 in pieces), gradient 14, 26
+// and 60 (33, 59 and 62), policy 31, 35 and 64 (85, 89 and 89); 65536 x 511 fp32 gradient 45
+// (55); but 65536 x 512 bf16 gradient 76 (40 in pieces): single bf16 elements
+// are stored two bytes at a time.
+bool short_rows(const pgc_logits* z) { return z->classes <= (z->dtype == PGC_BF16 ? 256 : 512); }
+unsigned short_grid(const pgc_logits* z) {
+  const int64_t rows = kWarps * (z->classes <= 128 ? 4 : z->classes <= 256 ? 2 : 1);
+  return (unsigned)((z->rows + rows - 1) / rows);
+}
+template <typename F>
+auto by_width(const pgc_logits* z, F f) {     // f.template operator()<E, L, R>()
+  const bool half = z->dtype == PGC_BF16;
+  if (z->classes <= 16) return half ? f.template operator()<__nv_bfloat16, 8, 2>() : f.template operator()<float, 8, 2>();
+  if (z->classes <= 64) return half ? f.template operator()<__nv_bfloat16, 8, 8>() : f.template operator()<float, 8, 8>();
+  if (z->classes <= 128) return half ? f.template operator()<__nv_bfloat16, 8, 16>() : f.template operator()<float, 8, 16>();
+  if (z->classes <= 256) return half ? f.template operator()<__nv_bfloat16, 16, 16>() : f.template operator()<float, 16, 16>();
+  return f.template operator()<float, 32, 16>();
+}
+struct ShortStats { template <typename E, int L, int R> auto operator()() { return short_stats_kernel<E, L, R>; } };
+struct ShortGrad { template <typename E, int L, int R> auto operator()() { return short_grad_kernel<E, L, R>; } };
+struct ShortPolicy { template <typename E, int L, int R> auto operator()() { return policy_short_kernel<E, L, R>; } };
+
 cudaError_t launch_stats(const pgc_logits* z, float* logp, float2* stats, Head* head, cudaStream_t st) {
   if (z->rows == 0) return cudaSuccess;
+  if (short_rows(z))
+    return launch(by_width(z, ShortStats()), short_grid(z), kThreads, 1, false, 0, st, rows_of(z), logp, stats, head);
   const Shape s = shape_of(z);
   const bool half = z->dtype == PGC_BF16;
   return launch(half ? s.warp ? row_stats_kernel<__nv_bfloat16, 32> : row_stats_kernel<__nv_bfloat16, kThreads>
@@ -784,6 +927,8 @@ cudaError_t launch_stats(const pgc_logits* z, float* logp, float2* stats, Head* 
 constexpr int64_t kGradPartBytes = 32 * 1024;
 cudaError_t launch_grad(const pgc_logits* z, const float* coef, const float2* stats, const Head* head, cudaStream_t st) {
   if (z->rows == 0) return cudaSuccess;
+  if (short_rows(z))
+    return launch(by_width(z, ShortGrad()), short_grid(z), kThreads, 1, head != nullptr, 0, st, rows_of(z), coef, stats, head);
   const Shape s = shape_of(z);
   const bool half = z->dtype == PGC_BF16;
   const int64_t bytes = z->classes * (half ? 2 : 4), most = INT32_MAX / z->rows;
@@ -825,6 +970,11 @@ cudaError_t allow_smem(const void* kernel, int which) {
 template <typename E>
 cudaError_t launch_policy(const pgc_logits* z, const Policy& p, cudaStream_t st) {
   const int64_t sms = sm_count(), pieces = z->classes / Elem<E>::N, bytes = pieces * 16;
+  if (short_rows(z)) {
+    const int64_t most = std::min<int64_t>(sms * 4, kMaxParts);
+    return launch(by_width(z, ShortPolicy()), (unsigned)std::max<int64_t>(std::min<int64_t>(short_grid(z), most), 1), kThreads, 1,
+                  true, 0, st, rows_of(z), p);
+  }
   const bool warp = bytes <= kHeldWarpBytes;
   int ranks = 1;
   if (!warp) {

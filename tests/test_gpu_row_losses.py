@@ -79,7 +79,8 @@ def check_gradient(torch, got, x, y, coef, tau, p, ep, ecoef, headroom=None):
     assert (err <= tol).all(), (np.argwhere(err > tol)[:5], (err / tol).max())
 
 
-SIZES = [(1, 1), (3, 2), (5, 7), (4, 8), (9, 33), (70, 100), (300, 10), (33, 1000), (6, 4095), (5, 4096), (4, 4097), (3, 8191),
+SIZES = [(1, 1), (3, 2), (5, 7), (4, 8), (9, 33), (70, 100), (300, 10), (31, 16), (66, 17), (37, 64), (5, 65), (35, 128), (18, 129),
+         (17, 256), (9, 257), (11, 512), (6, 513), (33, 1000), (6, 4095), (5, 4096), (4, 4097), (3, 8191),
          (3, 12345), (5, 32768), (3, 50001), (2, 131072), (1, 262147)]
 
 
@@ -137,7 +138,7 @@ def test_pitches_and_alignments(cuda, losses, dtype, T, V, pad, shift, out_pad, 
 
 def test_masked_logits_and_values(cuda, losses):
     torch = cuda
-    for V in (64, 6000, 40000):
+    for V in (64, 120, 400, 600, 6000, 40000):
         _, x, y = make(torch, torch.float32, 8, V, seed=2)
         y[:] = torch.arange(8, dtype=torch.int32) * (V // 9)
         x[0, 1:] = -float("inf")                    # one class left, the target
@@ -381,6 +382,11 @@ def away(drift, clip):
     (2, [30, 2], dict(kl=0.1, reduction="sequences")),
     (10, [400, 13, 1], dict(kl=0.05, clip=(0.1, 0.3), scale=2.0)),
     (257, [3, 0, 60], dict(reduction="sum", temperature=0.5)),
+    (16, [33, 5], dict(kl=0.2)),
+    (63, [37], dict(temperature=0.8)),
+    (120, [41, 1], dict(kl=0.1, reduction="sequences")),
+    (256, [19, 2], dict(kl=0.1)),
+    (500, [6, 11], dict(reduction="sequences")),
     (10, [1, 0, 2, 3] * 400, dict(kl=0.1, reduction="sequences")),
     (10, [40] * 130, dict(reduction="sequences")),
     (4099, [3, 4], dict(kl=0.3, reduction="sequences", temperature=1.5)),
