@@ -189,11 +189,25 @@ __device__ __forceinline__ float group_sum(float v) {
   for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-// A row's elements l, l + L, ... and -inf behind them (throughout, if not taken).
-template <typename E, int L, int R>
+// Which element a lane's j-th is: single ones, or (P = 2: bf16 rows of even
+// length and pitch that start on 4 bytes) two neighbours, read at once.
+template <int L, int P>
+__device__ __forceinline__ int short_at(int l, int j) { return P * (l + j / P * L) + j % P; }
+// A row's elements of lane l and -inf behind them (throughout, if not taken).
+template <typename E, int L, int P, int R>
 __device__ __forceinline__ void short_load(const E* x, int l, int V, bool taken, float (&v)[R]) {
 #pragma unroll
-  for (int j = 0; j < R; ++j) v[j] = taken && l + j * L < V ? Elem<E>::get(x + l + j * L) : -INFINITY;
+  for (int j = 0; j < R; j += P) {
+    const int e = short_at<L, P>(l, j);
+    if (P == 2) {
+      uint32_t w = Elem<E>::kLowest;
+      if (taken && e < V) w = *reinterpret_cast<const uint32_t*>(x + e);
+      v[j] = __uint_as_float(w << 16);
+      v[j + P - 1] = __uint_as_float(w & 0xffff0000u);
+    } else {
+      v[j] = taken && e < V ? Elem<E>::get(x + e) : -INFINITY;
+    }
+  }
 }
 // (m, sum) of a row, v becoming 2^((x - m) c).  All lanes of the warp take part.
 template <int L, int R>
@@ -211,18 +225,30 @@ __device__ __forceinline__ float2 short_exps(float (&v)[R], bool taken, float c)
   return make_float2(m, group_sum<L>(s));
 }
 // k ([v = y] - p) / tau of the row, where v times scale is p; 0 or NaN throughout with such a k.
-template <typename E, int L, int R>
+template <typename E, int L, int P, int R>
 __device__ __forceinline__ void short_store(E* g, int l, int V, const float (&v)[R], float scale, float k, float inv_tau, int y) {
-  const bool fill = k == 0.f || isnan(k);
+  const bool fill = k == 0.f || isnan(k), at_once = reinterpret_cast<uintptr_t>(g) % 4 == 0;
   const float at = k * inv_tau;
+  auto value = [&](int j, int e) { return fill ? k : fmaf(v[j] * scale, -at, e == y ? at : 0.f); };
 #pragma unroll
-  for (int j = 0; j < R; ++j) {
-    const int e = l + j * L;
-    if (e < V) Elem<E>::put(g + e, fill ? k : fmaf(v[j] * scale, -at, e == y ? at : 0.f));
+  for (int j = 0; j < R; j += P) {
+    const int e = short_at<L, P>(l, j);
+    if (e >= V) continue;
+    if constexpr (P == 2) {
+      const uint32_t w = Elem<E>::two(pair(value(j, e), value(j + 1, e + 1)));
+      if (at_once) {
+        *reinterpret_cast<uint32_t*>(g + e) = w;
+      } else {
+        reinterpret_cast<uint16_t*>(g)[e] = (uint16_t)w;
+        reinterpret_cast<uint16_t*>(g)[e + 1] = (uint16_t)(w >> 16);
+      }
+    } else {
+      Elem<E>::put(g + e, value(j, e));
+    }
   }
 }
 
-template <typename E, int L, int R>
+template <typename E, int L, int R, int P>
 __global__ void __launch_bounds__(kThreads) short_stats_kernel(Rows a, float* logp, float2* stats, Head* head) {
   const int lane = threadIdx.x % 32, l = lane % L;
   const int64_t t = (blockIdx.x * (int64_t)kWarps + threadIdx.x / 32) * (32 / L) + lane / L;
@@ -231,7 +257,7 @@ __global__ void __launch_bounds__(kThreads) short_stats_kernel(Rows a, float* lo
   const int32_t y = t < a.T ? a.y[t] : -1;
   const E* x = static_cast<const E*>(a.x) + t * a.ld;
   float v[R];
-  short_load<E, L>(x, l, a.V, y >= 0, v);
+  short_load<E, L, P>(x, l, a.V, y >= 0, v);
   const float xy = y >= 0 ? y < a.V ? Elem<E>::get(x + y) : NAN : 0.f;
   const float2 ms = short_exps<L>(v, y >= 0, a.c);
   if (l || t >= a.T) return;
@@ -240,21 +266,21 @@ __global__ void __launch_bounds__(kThreads) short_stats_kernel(Rows a, float* lo
   stats[t] = st;
 }
 
-template <typename E, int L, int R>
+template <typename E, int L, int R, int P>
 __global__ void __launch_bounds__(kThreads) short_grad_kernel(Rows a, const float* coef, const float2* stats, const Head* head) {
   const int lane = threadIdx.x % 32, l = lane % L;
   const int64_t t = (blockIdx.x * (int64_t)kWarps + threadIdx.x / 32) * (32 / L) + lane / L;
   if (t >= a.T) return;
   const int32_t y = a.y[t];
   float v[R];
-  short_load<E, L>(static_cast<const E*>(a.x) + t * a.ld, l, a.V, y >= 0, v);
+  short_load<E, L, P>(static_cast<const E*>(a.x) + t * a.ld, l, a.V, y >= 0, v);
   if (head) wait_for_previous();
   const bool bad = head && head->bad;
   const float k = bad || y >= a.V ? NAN : y < 0 ? 0.f : coef[t];
   const float2 st = y >= 0 ? stats[t] : make_float2(0.f, 0.f);
 #pragma unroll
   for (int j = 0; j < R; ++j) v[j] = ex2((v[j] - st.x) * a.c - st.y * kLog2e);
-  short_store<E, L>(static_cast<E*>(a.g) + t * a.ldg, l, a.V, v, 1.f, k, a.inv_tau, y);
+  short_store<E, L, P>(static_cast<E*>(a.g) + t * a.ldg, l, a.V, v, 1.f, k, a.inv_tau, y);
 }
 
 // ---- preference ------------------------------------------------------------
@@ -719,7 +745,7 @@ __global__ void __launch_bounds__(NT, 768 / NT) policy_held_kernel(Rows a, Polic
 }
 
 // Short rows: from and to memory through registers.
-template <typename E, int L, int R>
+template <typename E, int L, int R, int P>
 __global__ void __launch_bounds__(kThreads, 4) policy_short_kernel(Rows a, Policy p) {
   __shared__ Sum red[kWarps][3];
   __shared__ int2 counted;
@@ -734,7 +760,7 @@ __global__ void __launch_bounds__(kThreads, 4) policy_short_kernel(Rows a, Polic
     const int32_t y = t < a.T ? a.y[t] : -1;
     const RowIn in = row_in<E>(a, p, t, y);
     float v[R];
-    short_load<E, L>(static_cast<const E*>(a.x) + t * a.ld, l, a.V, y >= 0, v);
+    short_load<E, L, P>(static_cast<const E*>(a.x) + t * a.ld, l, a.V, y >= 0, v);
     const float2 ms = short_exps<L>(v, y >= 0, a.c);
     if (t >= a.T) continue;
     float coef = state.bad ? NAN : 0.f, lp = 0.f;
@@ -743,7 +769,7 @@ __global__ void __launch_bounds__(kThreads, 4) policy_short_kernel(Rows a, Polic
       coef = state.coefficient(a, p, in, lp, l == 0);
     }
     if (l == 0) p.logp[t] = lp;
-    if (a.g) short_store<E, L>(static_cast<E*>(a.g) + t * a.ldg, l, a.V, v, 1.f / ms.y, coef, a.inv_tau, y);
+    if (a.g) short_store<E, L, P>(static_cast<E*>(a.g) + t * a.ldg, l, a.V, v, 1.f / ms.y, coef, a.inv_tau, y);
   }
   __syncwarp();
   for (int j = 0; j < 3; ++j)
@@ -887,29 +913,41 @@ cudaError_t launch(void (*kernel)(P...), unsigned grid, int threads, int ranks, 
   return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
 }
 
-// Short rows: up to 128 classes by 8 lanes, 256 by 16, fp32 up to 512 by 32; rows
-// above are read in 16-byte pieces by a warp.  131072 rows of 10, 100 and 256 bf16
-// classes: forward 15, 14 and 25 us a call (36, 46 and 50 in pieces), gradient 14, 26
-// and 60 (33, 59 and 62), policy 31, 35 and 64 (85, 89 and 89); 65536 x 511 fp32 gradient 45
-// (55); but 65536 x 512 bf16 gradient 76 (40 in pieces): single bf16 elements
-// are stored two bytes at a time.
-bool short_rows(const pgc_logits* z) { return z->classes <= (z->dtype == PGC_BF16 ? 256 : 512); }
+// Rows of bf16 whose elements can be taken in pairs (whatever the gradient's
+// pitch: it does not change the results).
+bool in_pairs(const pgc_logits* z) { return z->classes % 2 == 0 && z->ld % 2 == 0 && (uintptr_t)z->x % 4 == 0; }
+// Short rows: up to 128 classes by 8 lanes, 256 by 16, 512 by 32 (fp32, and bf16 in
+// pairs); rows above are read in 16-byte pieces by a warp.  131072 rows of 10, 100 and 256 bf16
+// classes: forward 15, 14 and 21 us a call (36, 46 and 50 in pieces), gradient 14, 14
+// and 27 (33, 59 and 62), policy 31, 33 and 54 (85, 89 and 89); 65536 x 511 fp32 gradient 45 (55), x 512
+// bf16 27 (39).  Up to 1024 classes this way the policy loss turns: 74 us for 87040 x 1000 bf16, 64 in pieces.
+bool short_rows(const pgc_logits* z) { return z->classes <= (z->dtype == PGC_F32 || in_pairs(z) ? 512 : 256); }
 unsigned short_grid(const pgc_logits* z) {
   const int64_t rows = kWarps * (z->classes <= 128 ? 4 : z->classes <= 256 ? 2 : 1);
   return (unsigned)((z->rows + rows - 1) / rows);
 }
+// f.template operator()<E, L, R, P>()
 template <typename F>
-auto by_width(const pgc_logits* z, F f) {     // f.template operator()<E, L, R>()
-  const bool half = z->dtype == PGC_BF16;
-  if (z->classes <= 16) return half ? f.template operator()<__nv_bfloat16, 8, 2>() : f.template operator()<float, 8, 2>();
-  if (z->classes <= 64) return half ? f.template operator()<__nv_bfloat16, 8, 8>() : f.template operator()<float, 8, 8>();
-  if (z->classes <= 128) return half ? f.template operator()<__nv_bfloat16, 8, 16>() : f.template operator()<float, 8, 16>();
-  if (z->classes <= 256) return half ? f.template operator()<__nv_bfloat16, 16, 16>() : f.template operator()<float, 16, 16>();
-  return f.template operator()<float, 32, 16>();
+auto by_width(const pgc_logits* z, F f) {
+  const int64_t V = z->classes;
+  if (z->dtype == PGC_F32) {
+    if (V <= 16) return f.template operator()<float, 8, 2, 1>();
+    if (V <= 64) return f.template operator()<float, 8, 8, 1>();
+    if (V <= 128) return f.template operator()<float, 8, 16, 1>();
+    if (V <= 256) return f.template operator()<float, 16, 16, 1>();
+    return f.template operator()<float, 32, 16, 1>();
+  }
+  using H = __nv_bfloat16;
+  if (V <= 16) return f.template operator()<H, 8, 2, 1>();
+  const bool two = in_pairs(z);
+  if (V <= 64) return two ? f.template operator()<H, 8, 8, 2>() : f.template operator()<H, 8, 8, 1>();
+  if (V <= 128) return two ? f.template operator()<H, 8, 16, 2>() : f.template operator()<H, 8, 16, 1>();
+  if (V <= 256) return two ? f.template operator()<H, 16, 16, 2>() : f.template operator()<H, 16, 16, 1>();
+  return f.template operator()<H, 32, 16, 2>();
 }
-struct ShortStats { template <typename E, int L, int R> auto operator()() { return short_stats_kernel<E, L, R>; } };
-struct ShortGrad { template <typename E, int L, int R> auto operator()() { return short_grad_kernel<E, L, R>; } };
-struct ShortPolicy { template <typename E, int L, int R> auto operator()() { return policy_short_kernel<E, L, R>; } };
+struct ShortStats { template <typename E, int L, int R, int P> auto operator()() { return short_stats_kernel<E, L, R, P>; } };
+struct ShortGrad { template <typename E, int L, int R, int P> auto operator()() { return short_grad_kernel<E, L, R, P>; } };
+struct ShortPolicy { template <typename E, int L, int R, int P> auto operator()() { return policy_short_kernel<E, L, R, P>; } };
 
 cudaError_t launch_stats(const pgc_logits* z, float* logp, float2* stats, Head* head, cudaStream_t st) {
   if (z->rows == 0) return cudaSuccess;

@@ -80,7 +80,7 @@ def check_gradient(torch, got, x, y, coef, tau, p, ep, ecoef, headroom=None):
 
 
 SIZES = [(1, 1), (3, 2), (5, 7), (4, 8), (9, 33), (70, 100), (300, 10), (31, 16), (66, 17), (37, 64), (5, 65), (35, 128), (18, 129),
-         (17, 256), (9, 257), (11, 512), (6, 513), (33, 1000), (6, 4095), (5, 4096), (4, 4097), (3, 8191),
+         (17, 255), (17, 256), (9, 257), (9, 258), (11, 511), (11, 512), (6, 513), (6, 514), (33, 1000), (6, 4095), (5, 4096), (4, 4097), (3, 8191),
          (3, 12345), (5, 32768), (3, 50001), (2, 131072), (1, 262147)]
 
 
@@ -107,6 +107,7 @@ def test_token_logprob(cuda, losses, T, V, dtype, tau):
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 @pytest.mark.parametrize("T,V,pad,shift,out_pad,out_shift", [
     (7, 1000, 0, 1, 0, 1), (7, 1000, 8, 0, 0, 0), (7, 1001, 0, 3, 0, 3), (7, 1001, 5, 2, 2, 1), (5, 33, 1, 5, 3, 0),
+    (9, 100, 0, 1, 0, 1), (9, 100, 1, 0, 0, 0), (9, 100, 2, 2, 0, 1), (9, 300, 2, 0, 4, 2), (9, 300, 0, 1, 0, 0), (9, 60, 0, 0, 1, 0),
     (5, 20003, 0, 1, 0, 1), (5, 20003, 6, 3, 1, 2), (4, 70001, 0, 7, 0, 7), (4, 70001, 0, 7, 0, 0), (3, 5, 0, 1, 0, 2)])
 def test_pitches_and_alignments(cuda, losses, dtype, T, V, pad, shift, out_pad, out_shift):
     torch = cuda
