@@ -62,6 +62,17 @@ __device__ __forceinline__ int cluster_rank() {
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(n));
   return n;
 }
+// A CTA's shared memory may be written by another one of its cluster only once
+// it runs: every CTA says so (arrive), and knows it of all of them (wait) before its first store
+// to a neighbour.  All threads of the cluster call both, or neither.
+__device__ __forceinline__ void cluster_say_started(int ranks) {
+  if (ranks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait_started(int ranks) {
+  if (ranks <= 1) return;
+  __syncwarp();
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 
 // A row belongs to a warp (G = 32), or to the CTA, or the cluster of CTAs, of
 // the group's threads.  Exchanges alternate between two buffers, so that one
@@ -105,11 +116,15 @@ __device__ __forceinline__ Online merge(Online o, float c, Shared& sh, int& turn
 // Logarithm of a row's sum at its maximum.
 __device__ __forceinline__ float log_sum(const Online& o, float c) { return logf(o.s) - kLn2 * fmaf(o.m, c, -o.M); }
 
-// The row's largest logit and log sum, for all threads of the group.
+// The row's largest logit and log sum, for all threads of the group, or of the
+// cluster, which takes one row only.
 template <typename E, int G>
 __device__ __forceinline__ float2 row_stats(const E* x, const Slice& s, int tid, float c, Shared& sh, int& turn,
                                             int rank, int ranks) {
-  Online o = merge<G>(slice_stats<E, G, kUnroll>(x, s, tid, c), c, sh, turn, rank, ranks);
+  cluster_say_started(ranks);
+  Online o = slice_stats<E, G, kUnroll>(x, s, tid, c);
+  cluster_wait_started(ranks);
+  o = merge<G>(o, c, sh, turn, rank, ranks);
   if (!is_extreme(o.m, c)) return make_float2(o.m, log_sum(o, c));
   Online q;
   q.M = 0.f;
@@ -674,6 +689,7 @@ __global__ void __launch_bounds__(NT, 768 / NT) policy_held_kernel(Rows a, Polic
   int64_t t = kWarpRow ? blockIdx.x * (int64_t)(NT / 32) + threadIdx.x / 32 : blockIdx.x / ranks;
   const uint32_t at = smem_u32(rows_smem) + (kWarpRow ? (threadIdx.x / 32) * most * G * 16 : 0);
   int turn = 0;
+  cluster_say_started(ranks);
   PolicyState state;
   const E* x = static_cast<const E*>(a.x) + t * a.ld;
   E* g = static_cast<E*>(a.g) + t * a.ldg;
@@ -686,6 +702,7 @@ __global__ void __launch_bounds__(NT, 768 / NT) policy_held_kernel(Rows a, Polic
     copy_row<E, G>(row, at, tid, most);
   }
   state.weigh(p, counted);
+  cluster_wait_started(ranks);
   RowIn in{-1, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (scalars) in = row_in<E>(a, p, t, y);
   for (; t < a.T; t += groups, x += x_step, g += g_step) {
@@ -791,8 +808,10 @@ __global__ void __launch_bounds__(kLongThreads, 1) policy_long_kernel(Rows a, Po
   const int tid = threadIdx.x;
   const bool scalars = tid < 32, first = tid == 0 && rank == 0;
   int turn = 0;
+  cluster_say_started(ranks);
   PolicyState state;
   state.weigh(p, counted);
+  cluster_wait_started(ranks);
   const int64_t groups = gridDim.x / ranks;
   for (int64_t t = blockIdx.x / ranks; t < a.T; t += groups) {
     const int32_t y = a.y[t];

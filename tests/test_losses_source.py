@@ -1,0 +1,34 @@
+"""What the kernels of the losses on rows must hold and no run can show: read
+from their sources, without a GPU."""
+
+import os
+import re
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2607_20739_gb300", "csrc")
+
+
+def functions(name):
+    """{function: body} of a source file, comments left out."""
+    with open(os.path.join(CSRC, name)) as f:
+        text = re.sub(r"//[^\n]*|__launch_bounds__\([^()]*\)", "", f.read())
+    out = {}
+    for m in re.finditer(r"\b(\w+)\([^;{}]*\)\s*\{\n", text):
+        depth, at = 1, m.end()
+        while depth:
+            depth += {"{": 1, "}": -1}.get(text[at], 0)
+            at += 1
+        out[m.group(1)] = text[m.end():at]
+    return out
+
+
+def test_clusters_have_started_before_they_are_written():
+    """A store to another CTA's shared memory needs that CTA to run: behind
+    the barrier that every CTA of the cluster reaches at its start."""
+    body = functions("row_losses.cu")
+    exchanges = [f for f in body if "st.shared::cluster" in body[f]]
+    assert sorted(exchanges) == ["gather", "merge"]
+    callers = [f for f in body if re.search(r"\b(gather|merge)<", body[f])]
+    assert sorted(callers) == ["policy_held_kernel", "policy_long_kernel", "row_stats"]
+    for f in callers:
+        say, wait = body[f].index("cluster_say_started("), body[f].index("cluster_wait_started(")
+        assert say < wait < re.search(r"\b(gather|merge)<", body[f]).start(), f
