@@ -128,7 +128,7 @@ __device__ __forceinline__ float2 row_stats(const E* x, const Slice& s, int tid,
   if (!is_extreme(o.m, c)) return make_float2(o.m, log_sum(o, c));
   Online q;
   q.M = 0.f;
-  for (int v = s.first + tid; v < s.last; v += G) q.s += exp2f((Elem<E>::get(x + v) - o.m) * c);
+  for (unsigned v = s.first + tid; v < (unsigned)s.last; v += G) q.s += exp2f((Elem<E>::get(x + v) - o.m) * c);
   q.m = 0.f;
   return make_float2(o.m, logf(merge<G>(q, c, sh, turn, rank, ranks).s));
 }
@@ -838,7 +838,7 @@ __global__ void __launch_bounds__(kLongThreads, 1) policy_long_kernel(Rows a, Po
       if (q.kind == kExtremeSum) {
         Online e;
         e.m = e.M = 0.f;
-        for (int v = s.first + tid; v < s.last; v += G) e.s += exp2f((Elem<E>::get(x + v) - q.m) * a.c);
+        for (unsigned v = s.first + tid; v < (unsigned)s.last; v += G) e.s += exp2f((Elem<E>::get(x + v) - q.m) * a.c);
         e = gather<G>(e, a.c, sh, turn, rank, ranks);
         if (scalars) q = work_out(a, p, state, in, o.m, logf(e.s), kExtreme, t, first);
         publish();

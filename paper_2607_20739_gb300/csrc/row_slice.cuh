@@ -156,7 +156,9 @@ __device__ __forceinline__ uint4 load16(const uint4* p) { return __ldcg(p); }
 __device__ __forceinline__ void store16(uint4* p, const uint4& v) { __stcs(p, v); }
 
 // Elements [first, last) of a row: `head` single ones up to a 16-byte
-// boundary, pieces, and a rest behind them.
+// boundary, pieces, and a rest behind them.  A row has up to 2^31 - 1 elements:
+// an index of single elements that steps beyond the last one is unsigned, as
+// int would turn negative there; pieces are at most 2^29.
 struct Slice {
   int first, last, head, pieces;
 };
@@ -286,9 +288,9 @@ __device__ __forceinline__ void slice_fill(E* g, int first, int last, int tid, f
 
 template <typename E>
 __device__ __noinline__ void slice_grad_extreme(const E* x, E* g, int first, int last, int tid, int threads, RowGrad r) {
-  for (int v = first + tid; v < last; v += threads) {
+  for (unsigned v = first + tid; v < (unsigned)last; v += threads) {
     const float p = exp2f((Elem<E>::get(x + v) - r.m) * r.c - r.l2);
-    Elem<E>::put(g + v, r.k * p + (v == r.y ? r.at_y : 0.f));
+    Elem<E>::put(g + v, r.k * p + ((int)v == r.y ? r.at_y : 0.f));
   }
 }
 

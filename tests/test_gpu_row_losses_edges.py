@@ -36,3 +36,24 @@ def test_rows_split_over_clusters(cuda, losses, dtype, T, V):
         same &= (again[0] == logp).all() & (again[1] == stats).all() & (twice["dlogits"] == pol["dlogits"]).all()
         same &= (twice["logp"] == pol["logp"]).all() & (twice["loss"] == pol["loss"])
     assert bool(same)
+
+
+def test_longest_row(cuda, losses):
+    """A row of 2^31 - 1 classes, all masked by the lowest value, so that every
+    pass goes element by element (bf16: 4.3 GB, written in place)."""
+    torch = cuda
+    V = (1 << 31) - 1
+    low = float(torch.finfo(torch.bfloat16).min)
+    x = torch.full((1, V), low, dtype=torch.bfloat16, device="cuda")
+    y = torch.tensor([V - 1], dtype=torch.int32, device="cuda")
+    logp, stats = losses.token_logprob(x, y)
+    # equal terms: sums of ones below 2^24 per thread are exact, their total is rounded, log within 2 u
+    assert float(logp) == pytest.approx(-np.log(V), rel=4 * U)
+    one = torch.ones(1, device="cuda")
+    p = torch.tensor(-1.0 / V).bfloat16()           # 2^-31 (1 + 2^-31): one bf16 value, its neighbours 2^-8 away
+    d = losses.token_logprob_grad(x, y, stats, one, out=x)
+    assert (d[0, :V - 1] == p.cuda()).all() and float(d[0, V - 1]) == 1.0
+    x.fill_(low)
+    pol = losses.policy_loss(x, y, logp, -one, out=x)
+    assert torch.equal(pol["logp"], logp) and float(pol["loss"]) == 1.0
+    assert (x[0, :V - 1] == p.cuda()).all() and float(x[0, V - 1]) == 1.0

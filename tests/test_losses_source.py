@@ -32,3 +32,20 @@ def test_clusters_have_started_before_they_are_written():
     for f in callers:
         say, wait = body[f].index("cluster_say_started("), body[f].index("cluster_wait_started(")
         assert say < wait < re.search(r"\b(gather|merge)<", body[f]).start(), f
+
+
+def test_indexes_of_elements_do_not_overflow():
+    """A row may have 2^31 - 1 classes, so an index that steps through its single
+    elements by the threads of a group passes 2^31 before the loop's test."""
+    loops = []
+    for name in ("row_losses.cu", "row_slice.cuh"):
+        for f, body in functions(name).items():
+            loops += [(f, t) for t, bound in re.findall(r"for \((\w+) \w+ = [^;]*tid; \w+ < ([^;]*); \w+ \+= (?:G|threads)\)", body)
+                      if "last" in bound]
+    assert {f for f, _ in loops} == {"row_stats", "policy_long_kernel", "slice_grad_extreme"}
+    step = 1024
+    for f, kind in loops:
+        last = (1 << 31) - 1
+        beyond = last - 1 + step                    # the last element's thread, one step on
+        wrapped = {"int": (beyond + (1 << 31)) % (1 << 32) - (1 << 31), "unsigned": beyond % (1 << 32), "int64_t": beyond}[kind]
+        assert wrapped >= last, f
