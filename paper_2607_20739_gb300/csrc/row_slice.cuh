@@ -5,10 +5,12 @@
 // Exponents are base 2 with c = log2(e) / tau: 2^(x c - M) for the float
 // M = fl(m c).  x c - M is one FMA, rounded once; that M is not m c itself
 // does no harm, as any M close to it serves: its residue r = m c - M (exact,
-// one FMA) is taken out of the logarithm of the sum.  M is held above -1e38, so that a
-// thread that has met nothing but -inf (or the type's lowest value, as masks
-// write it) adds 0 instead of NaN; a whole row of such values, or one of very
-// large products, is `extreme` and goes through (x - m) c in place of it.
+// one FMA) is taken out of the logarithm of the sum.  M is held above -1e8: down to
+// there the residue is below 2^3, further down it would pass the range of 2^x.  A
+// thread that has met nothing above -1e8 (-inf, or the large negative
+// numbers that masks write) adds 2^(x c + 1e8), which is 0 or at most 2^3, and its sum is valid for that
+// M; a whole row of such values, or one of products above 1e8, is `extreme` and
+// goes through (x - m) c in place of it.
 #pragma once
 
 #include "dev_common.cuh"
@@ -180,11 +182,12 @@ __device__ __forceinline__ Slice slice_of(const E* x, int n, int rank, int ranks
   return s;
 }
 
-// Running maximum and sum: s = sum of 2^(x c - M), M = max(fl(m c), -1e38).
+// Running maximum and sum: s = sum of 2^(x c - M), M = max(fl(m c), -kFar).
+constexpr float kFar = 1e8f;
 struct Online {
-  float m = -INFINITY, M = -1e38f, s = 0.f;
+  float m = -INFINITY, M = -kFar, s = 0.f;
 };
-__device__ __forceinline__ float ref_of(float m, float c) { return fmaxf(m * c, -1e38f); }
+__device__ __forceinline__ float ref_of(float m, float c) { return fmaxf(m * c, -kFar); }
 __device__ __forceinline__ void raise(Online& o, float top, float c) {
   if (top > o.m) {
     const float M = ref_of(top, c);
@@ -252,9 +255,9 @@ struct RowGrad {
   float l2;       // log2 of the sum at m (extreme rows)
   float k;        // -coef / tau (extreme rows)
 };
-// A row whose largest logit leaves the range of the fast path: up to |m c| = 1e8
-// the residue m c - M is below 2^3, beyond it 2^residue would soon overflow.
-__device__ __forceinline__ bool is_extreme(float m, float c) { return !(fabsf(m) < 1e37f && fabsf(m * c) < 1e8f); }
+// A row whose largest logit leaves the range of the fast path: beyond kFar
+// 2^(residue of m c) would soon overflow, and M is no longer fl(m c).
+__device__ __forceinline__ bool is_extreme(float m, float c) { return !(fabsf(m) < 1e37f && fabsf(m * c) < kFar); }
 
 __device__ __forceinline__ RowGrad row_grad(float m, float L, float coef, float inv_tau, float c, int y) {
   RowGrad g;

@@ -4,7 +4,9 @@ from zero, against the 64-bit oracle (bounds: test_gpu_row_losses.py)."""
 import numpy as np
 import pytest
 
-from test_gpu_row_losses import U, check_gradient, check_policy, losses, make, on_host, rows_and_bounds  # noqa: F401
+from oracle import row_losses_oracle as O
+from test_gpu_row_losses import (U, check_gradient, check_policy, check_preference, losses, make, offsets_of,  # noqa: F401
+                                 on_host, rows_and_bounds)
 
 pytestmark = pytest.mark.gpu
 
@@ -57,3 +59,61 @@ def test_longest_row(cuda, losses):
     pol = losses.policy_loss(x, y, logp, -one, out=x)
     assert torch.equal(pol["logp"], logp) and float(pol["loss"]) == 1.0
     assert (x[0, :V - 1] == p.cuda()).all() and float(x[0, V - 1]) == 1.0
+
+
+MASKS = [-1e4, -1e9, -5e9, -1e10, -1e20, -1e30, -1e37, "lowest"]
+
+
+def masked_rows(torch, dtype, V, seed):
+    """A row for every mask value and place of the masked classes: a prefix, a suffix, all but ten, the last one
+    alone, every second (by -inf and the value in turn), and all of them."""
+    places = 6
+    r, x, y = make(torch, dtype, places * len(MASKS), V, seed=seed)
+    for i, value in enumerate(MASKS):
+        value = float(torch.finfo(dtype).min) if value == "lowest" else value
+        rows = range(places * i, places * (i + 1))
+        x[rows[0], :V // 2] = value
+        x[rows[1], V // 5:] = value
+        keep = x[rows[2], V // 3:V // 3 + 10].clone()
+        x[rows[2]] = value
+        x[rows[2], V // 3:V // 3 + 10] = keep
+        x[rows[3], V - 1] = value
+        x[rows[4], 1::2] = value
+        x[rows[4], 1::4] = -float("inf")
+        x[rows[5]] = value
+        for row, at in zip(rows, (V - 1, 0, V // 3 + 4, V // 7, V // 4 * 2, 3)):
+            y[row] = at
+    return r, x, y
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("V", [100, 500, 600, 1000, 1001, 9001, 20003, 50001, 70001, 131073])
+def test_masks_of_any_value(cuda, losses, dtype, V):
+    """Classes masked by large negative numbers count for nothing, whatever the number, the temperature and the
+    order in which a thread meets them.  (Elements of probability 0 are exact, so the bounds are those of the rest.)"""
+    torch = cuda
+    r, x, y = masked_rows(torch, getattr(torch, dtype), V, 29)
+    T = len(y)
+    copies = 4                                      # enough rows that none is split over a cluster, and a few to a CTA
+    many, ymany = x.repeat(copies, 1), y.repeat(copies)
+    off, off_d = offsets_of(torch, [T // 2, T - T // 2])
+    one = torch.ones(T, device="cuda")
+    for tau in (0.6, 0.7, 1.0, 1.3, 10.0):
+        logp, stats = losses.token_logprob(x, y, tau)
+        want, m, L, p, elogp, ep = rows_and_bounds(x, y, tau)
+        assert (np.abs(on_host(logp) - want) <= elogp).all(), tau
+        assert (np.abs(on_host(stats)[:, 1] - L) <= elogp).all()
+        d = losses.token_logprob_grad(x, y, stats, one, tau)
+        check_gradient(torch, d, x, y, np.ones(T), tau, p, ep, 0.0)
+        again, _ = losses.token_logprob(many, ymany, tau)
+        assert (np.abs(on_host(again).reshape(copies, T) - want) <= elogp).all()
+        old = torch.from_numpy((want - 0.1).astype(np.float32)).cuda()
+        pol = losses.policy_loss(x, y, old, one, temperature=tau)
+        check_policy(torch, pol, x, y, old, one, None, dict(temperature=tau))
+        all_of_them = losses.policy_loss(many, ymany, old.repeat(copies), one.repeat(copies), temperature=tau, scale=copies)
+        parts = all_of_them["dlogits"].view(copies, T, V)
+        assert (parts[1:] == parts[0]).all()
+        few = dict(pol, logp=all_of_them["logp"][:T], dlogits=parts[0])
+        check_policy(torch, few, x, y, old, one, None, dict(temperature=tau))
+        kw = dict(beta=0.01, average=True, temperature=tau)
+        check_preference(torch, losses.preference_loss(x, y, off_d, **kw), x, y, off, None, kw)
