@@ -59,7 +59,7 @@ def preference(x, y, off, ref=None, beta=0.1, kind="sigmoid", margin=0.0, smooth
         e = smoothing
         if kind == "sigmoid":
             f = (1 - e) * np.logaddexp(0, -h) + e * np.logaddexp(0, h)
-            df = 1 / (1 + np.exp(-h)) - (1 - e)
+            df = e * np.exp(-np.logaddexp(0, -h)) - (1 - e) * np.exp(-np.logaddexp(0, h))     # e sig(h) - (1 - e) sig(-h)
         elif kind == "hinge":
             f = (1 - e) * max(0.0, 1 - h) + e * max(0.0, 1 + h)
             df = e * (h > -1) - (1 - e) * (h < 1)

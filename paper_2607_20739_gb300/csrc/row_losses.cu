@@ -329,8 +329,11 @@ __device__ float pref_loss(const Pref& a, float gap, float* slope) {
     return h;
   }
   if (a.kind == PGC_PREF_SIGMOID) {
-    const float soft = log1pf(expf(-fabsf(h)));
-    *slope = beta * (1.f / (1.f + expf(-h)) - (1.f - e));
+    // e sig(h) - (1 - e) sig(-h): both from exp(-|h|), so that the one near 0 keeps its
+    // digits (sig(h) - (1 - e) has none left at h = 17, where a pair still moves a little)
+    const float t = expf(-fabsf(h)), soft = log1pf(t);
+    const float near = 1.f / (1.f + t), far = t / (1.f + t);
+    *slope = beta * (e * (h < 0.f ? far : near) - (1.f - e) * (h < 0.f ? near : far));
     return both(soft + fmaxf(-h, 0.f), soft + fmaxf(h, 0.f));
   }
   if (a.kind == PGC_PREF_HINGE) {

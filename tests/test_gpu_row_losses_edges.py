@@ -117,3 +117,39 @@ def test_masks_of_any_value(cuda, losses, dtype, V):
         check_policy(torch, few, x, y, old, one, None, dict(temperature=tau))
         kw = dict(beta=0.01, average=True, temperature=tau)
         check_preference(torch, losses.preference_loss(x, y, off_d, **kw), x, y, off, None, kw)
+
+
+@pytest.mark.parametrize("smoothing", [0.0, 0.1])
+@pytest.mark.parametrize("average", [False, True])
+def test_preference_of_well_separated_pairs(cuda, losses, smoothing, average):
+    """The slope of the sigmoid loss keeps its digits where it is small: relative to e sig(h) + (1 - e) sig(-h), the
+    sum of its two terms, exp is good to 4 u, and one sum, one quotient and the products with e, beta, scale, 1 /
+    pairs and 1 / rows add 7 u at most; h moves it by sig'(h) beta times the error of the gap, which is that of
+    the scores, its own rounding and, through h = beta gap, two more."""
+    torch = cuda
+    wanted = [-40.0, -20.0, -10.0, -5.0, -1.0, 0.3, 2.2, 5.0, 10.0, 12.0, 15.0, 17.0, 20.0, 40.0]
+    beta, pairs, rows = float(np.float32(0.1)), len(wanted), 3
+    T, V = 2 * pairs * rows, 1000
+    r, x, y = make(torch, torch.float32, T, V, seed=41)
+    off, off_d = offsets_of(torch, [rows] * (2 * pairs))
+    _, _, _, p, elogp, ep = rows_and_bounds(x, y, 1.0)
+    kw = dict(beta=beta, smoothing=float(np.float32(smoothing)), average=average)
+    scores = O.preference(on_host(x), y.cpu().numpy(), off, **kw)[1]
+    ref = np.zeros((pairs, 2))
+    ref[:, 1] = scores[:, 1] + 0.25
+    ref[:, 0] = scores[:, 0] - np.array(wanted) / beta + 0.25
+    ref = torch.from_numpy(ref.astype(np.float32)).cuda()
+    loss, scores, coef = O.preference(on_host(x), y.cpu().numpy(), off, ref.cpu().numpy(), **kw)
+    gap = (scores[:, 0] - scores[:, 1]) - (on_host(ref)[:, 0] - on_host(ref)[:, 1])
+    h = beta * gap
+    assert np.abs(h - wanted).max() < 1e-4
+    share = 1.0 / rows if average else 1.0
+    egap = (elogp.reshape(pairs, -1).sum(1) + 2 * U * np.abs(scores).sum(1)) * share + 3 * U * np.abs(gap)
+    near, far = 1 / (1 + np.exp(-h)), 1 / (1 + np.exp(h))
+    e = kw["smoothing"]
+    ecoef = beta * share / pairs * (1.01 * beta * near * far * egap + 11 * U * (e * near + (1 - e) * far))
+    res = losses.preference_loss(x, y, off_d, ref, **kw)
+    check_gradient(torch, res["dlogits"], x, y, coef, 1.0, p, ep, np.repeat(ecoef, 2 * rows))
+    value = (1 - e) * np.logaddexp(0, -h) + e * np.logaddexp(0, h)
+    eloss = np.mean(np.abs(e * near - (1 - e) * far) * beta * egap + 12 * U * value)
+    assert abs(float(res["loss"]) - loss) <= eloss
