@@ -106,8 +106,8 @@ def policy(x, y, old, adv, ref=None, clip=(0.2, 0.2), kl=0.0, off=None, reductio
         slope = 0.0 if clipped else -r * A
         if ref is not None:
             u = float(ref[t]) - logp[t]
-            terms[1] += w[t] * (np.exp(u) - u - 1)
-            slope += kl * (1 - np.exp(u))
+            terms[1] += w[t] * (np.expm1(u) - u)
+            slope -= kl * np.expm1(u)
         coef[t] = scale * w[t] * slope
     return scale * (terms[0] + kl * terms[1]), terms, logp, coef
 

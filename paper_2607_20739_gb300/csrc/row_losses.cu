@@ -534,6 +534,22 @@ __device__ __forceinline__ RowIn row_in(const Rows& a, const Policy& p, int64_t 
   return r;
 }
 
+// exp(u) - u - 1 with em = exp(u) - 1.  Near the reference policy, where training
+// starts, it is about u^2 / 2 and em - u has few digits left (none below u = 3e-4): there the Taylor series
+// u^2 (1/2! + u/3! + ... + u^6/8!), whose rest is below 2^-24 of it up to |u| = 1/2.
+__device__ __forceinline__ float kl_of(float u, float em) {
+  if (isinf(em)) return em;
+  if (!(fabsf(u) < 0.5f)) return em - u;
+  float s = 1.f / 40320.f;
+  s = fmaf(s, u, 1.f / 5040.f);
+  s = fmaf(s, u, 1.f / 720.f);
+  s = fmaf(s, u, 1.f / 120.f);
+  s = fmaf(s, u, 1.f / 24.f);
+  s = fmaf(s, u, 1.f / 6.f);
+  s = fmaf(s, u, 0.5f);
+  return s * u * u;
+}
+
 // The scalars of the policy loss: the rows' weights, of the counts that the
 // kernel before has taken, a row's part of the sums and its coefficient.
 struct PolicyState {
@@ -571,9 +587,9 @@ struct PolicyState {
     const float f = A == 0.f && !isnan(r) ? 0.f : free ? -r * A : -rc * A;
     float slope = free ? f : 0.f, kl = 0.f;
     if (p.ref_logp) {
-      const float away = in.ref - lp, ex = expf(away);
-      kl = isinf(ex) ? ex : ex - away - 1.f;
-      if (p.kl != 0.f) slope += p.kl * (1.f - ex);
+      const float away = in.ref - lp, em = expm1f(away);
+      kl = kl_of(away, em);
+      if (p.kl != 0.f) slope -= p.kl * em;
     }
     if (first) {
       sum[0].add(w * f);

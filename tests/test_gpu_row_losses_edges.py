@@ -153,3 +153,30 @@ def test_preference_of_well_separated_pairs(cuda, losses, smoothing, average):
     value = (1 - e) * np.logaddexp(0, -h) + e * np.logaddexp(0, h)
     eloss = np.mean(np.abs(e * near - (1 - e) * far) * beta * egap + 12 * U * value)
     assert abs(float(res["loss"]) - loss) <= eloss
+
+
+@pytest.mark.parametrize("V", [8, 1000, 20003, 70001])
+def test_policy_near_its_reference(cuda, losses, V):
+    """KL and its slope keep their digits where policy and reference nearly agree.  Both are functions of u = ref -
+    logp, so they are taken at the log probabilities that the call returned: u is one rounding off (none, where
+    small), which moves exp(u) - u - 1 by at most (2 + |u|) u of itself and exp(u) - 1 by (1 + |u|) u; exp(u) - 1
+    is good to 2 u; its distance to u to 9 u at |u| = 1/2 and better beyond, the series below to 6 u; weights,
+    coefficients and sums add 4 roundings."""
+    torch = cuda
+    T = 6
+    r, x, y = make(torch, torch.float32, T, V, seed=43, spread=1.0)
+    _, _, _, p, _, ep = rows_and_bounds(x, y, 1.0)
+    logp, _ = losses.token_logprob(x, y)
+    nothing = torch.zeros(T, device="cuda")
+    for size in (1e-5, 1e-4, 3e-4, 1e-3, 1e-2, 0.1, 0.3, 0.49, 0.51, 1.0, 3.0, 20.0):
+        for sign in (1, -1):
+            ref = logp + torch.from_numpy((sign * size * r.uniform(0.9, 1.0, T)).astype(np.float32)).cuda()
+            res = losses.policy_loss(x, y, logp, nothing, ref, kl=1.0)
+            u = on_host(ref) - on_host(res["logp"])
+            assert (np.sign(u) == sign).all()
+            kl = np.where(np.abs(u) < 1e-2, u * u * (1 / 2 + u / 6 * (1 + u / 4 * (1 + u / 5 * (1 + u / 6)))), np.expm1(u) - u)
+            tol = U * ((15 + np.abs(u)) * kl).mean()
+            assert abs(float(res["terms"][1]) - kl.mean()) <= tol, (size, sign)
+            assert abs(float(res["loss"]) - kl.mean()) <= tol + 2 * U * kl.mean()
+            coef = -np.expm1(u) / T
+            check_gradient(torch, res["dlogits"], x, y, coef, 1.0, p, ep, U * (7 + np.abs(u)) * np.abs(coef))
