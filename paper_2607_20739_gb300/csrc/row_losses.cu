@@ -315,12 +315,13 @@ struct Pref {
   Head* head;
 };
 
-// Loss of one pair's gap of log ratios, and its derivative.  A branch of
+// Loss of one pair's gap of log ratios, and its derivative (squared: of the gap
+// less margin / beta, which for a small beta only this kind has to hold).  A branch of
 // weight 0 takes no part, so that an infinite gap (an answer that the model
 // cannot give) has the loss and slope of its limit.
 __device__ float pref_loss(const Pref& a, float gap, float* slope) {
   const float beta = a.beta, e = a.smoothing;
-  const float h = beta * gap;
+  const float h = fmaf(beta, gap, -a.margin);
   auto both = [e](float chosen, float rejected) {      // (1 - e) chosen + e rejected
     return (e < 1.f ? (1.f - e) * chosen : 0.f) + (e > 0.f ? e * rejected : 0.f);
   };
@@ -399,7 +400,7 @@ __device__ __forceinline__ float2 finish_pair(const Pref& a, int64_t i, const in
     gap.add(-a.ref[2 * i]);
     gap.add(a.ref[2 * i + 1]);
   }
-  gap.add(-a.margin / a.beta);
+  if (a.kind == PGC_PREF_SQUARED) gap.add(-a.margin / a.beta);
   float slope;
   const float loss = pref_loss(a, gap.value(), &slope);
   if (lane == 0) a.pair_loss[i] = loss;

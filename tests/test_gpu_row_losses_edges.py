@@ -180,3 +180,20 @@ def test_policy_near_its_reference(cuda, losses, V):
             assert abs(float(res["loss"]) - kl.mean()) <= tol + 2 * U * kl.mean()
             coef = -np.expm1(u) / T
             check_gradient(torch, res["dlogits"], x, y, coef, 1.0, p, ep, U * (7 + np.abs(u)) * np.abs(coef))
+
+
+@pytest.mark.parametrize("kind", ["sigmoid", "hinge"])
+@pytest.mark.parametrize("beta", [1e-3, 1e-30, 1e-38])
+def test_preference_of_small_beta_and_margin(cuda, losses, kind, beta):
+    """h = beta gap - margin where margin / beta passes the range of a float: h is -margin to a rounding, and
+    everything is the function of it (4 u of exp, 4 more roundings)."""
+    torch = cuda
+    _, x, y = make(torch, torch.float32, 8, 50, seed=3)
+    off = torch.arange(9, dtype=torch.int32, device="cuda")
+    margin = 30.0
+    res = losses.preference_loss(x, y, off, kind=kind, beta=beta, margin=margin, smoothing=0.25)
+    loss = O.preference(on_host(x), y.cpu().numpy(), np.arange(9), beta=float(np.float32(beta)), kind=kind, margin=margin,
+                        smoothing=0.25)[0]
+    # beta gap (below 0.03) has the scores' error, 100 u at most here, times beta
+    assert float(res["loss"]) == pytest.approx(loss, rel=16 * U)
+    assert res["dlogits"].isfinite().all()
