@@ -197,3 +197,93 @@ def test_preference_of_small_beta_and_margin(cuda, losses, kind, beta):
     # beta gap (below 0.03) has the scores' error, 100 u at most here, times beta
     assert float(res["loss"]) == pytest.approx(loss, rel=16 * U)
     assert res["dlogits"].isfinite().all()
+
+
+def gradient_and_bound(torch, dtype, x, y, coef, p, ep, ecoef):
+    """coef ([v = y] - p) in double and check_gradient's bound, on the GPU (temperature 1, every row with a target)."""
+    ys = y.cpu().numpy()
+    want = O.logits_gradient(on_host(x), ys, coef)
+    one = np.zeros_like(p)
+    one[np.arange(len(ys)), ys] = 1.0
+    h = torch.finfo(dtype).eps / 2
+    k, ek = np.abs(coef)[:, None], ecoef[:, None]
+    tol = ((k + ek) * (p * ep + 4 * U * (one + p)) + ek * np.abs(one - p) + h * np.abs(want)) * (1 + h) + 1e-37
+    return torch.from_numpy(want).cuda(), torch.from_numpy(tol).cuda()
+
+
+MANY = [("bfloat16", 1001, 9000), ("bfloat16", 6144, 8000), ("bfloat16", 6152, 6000), ("bfloat16", 16385, 3000),
+        ("bfloat16", 18432, 2500), ("bfloat16", 18441, 2500), ("bfloat16", 32769, 1500), ("bfloat16", 56320, 1000),
+        ("bfloat16", 56329, 700), ("bfloat16", 65537, 700), ("bfloat16", 75776, 500), ("bfloat16", 75785, 500),
+        ("bfloat16", 100003, 500), ("bfloat16", 106496, 400), ("bfloat16", 106505, 400), ("bfloat16", 131073, 400),
+        ("float32", 1001, 9000), ("float32", 9001, 3000), ("float32", 20003, 1200), ("float32", 36001, 600),
+        ("float32", 50001, 400), ("float32", 53248, 400), ("float32", 53253, 400)]
+
+
+@pytest.mark.parametrize("dtype,V,T", MANY)
+def test_policy_of_many_rows(cuda, losses, dtype, V, T):
+    """Several rows to a CTA, one behind the other: 37 kinds of rows in turn, at every place in a 16-byte piece, so
+    that no row stands where one of its kind stood before; some without a target (alone, and more in a run than
+    there are CTAs), some clipped, some worked out element by element.  Every row against the oracle's row of its
+    kind; the same bits whatever the output's place."""
+    torch = cuda
+    kinds = 37
+    dtype = getattr(torch, dtype)
+    pad = V % 3
+    r, x, y = make(torch, dtype, kinds, V, seed=51, pad=pad, shift=1)
+    x[5] = float(torch.finfo(dtype).min)
+    x[9, V // 2:] = -1e10
+    x[11] += 3e4
+    x[12] = -1e30
+    y[9] = V // 3
+    logp, _, _, p, elogp, ep = rows_and_bounds(x, y, 1.0)
+    old = (logp - np.where(r.random(kinds) < 0.3, 0.5, 0.1)).astype(np.float32)
+    ref = (logp + 0.3 * r.standard_normal(kinds)).astype(np.float32)
+    adv = r.standard_normal(kinds).astype(np.float32)
+    kl = float(np.float32(0.1))
+    one = [O.policy(on_host(x[j:j + 1]), y[j:j + 1].cpu().numpy(), old[j:j + 1], adv[j:j + 1], ref[j:j + 1],
+                    reduction="sum", kl=kl) for j in range(kinds)]
+    terms, coef = np.array([o[1] for o in one]), np.array([o[3][0] for o in one])
+    # the ratio: logp's error and the difference's rounding in the exponent, 4 u of expf and the product; KL: by its derivative
+    A, ratio, u = np.abs(adv), np.exp(logp - old), ref - logp
+    er, eu = elogp + U * (np.abs(logp - old) + 6), elogp + U * np.abs(u)
+    ekl = np.abs(np.expm1(u)) * eu + eu ** 2 + 16 * U * terms[:, 1]
+    ecoef = A * ratio * er + kl * np.exp(u) * eu + 8 * U * (A * ratio + kl * np.abs(np.expm1(u)))
+    want, tol = gradient_and_bound(torch, dtype, x, y, coef, p, ep, ecoef)
+
+    kind = torch.arange(T, device="cuda") % kinds
+    store = torch.zeros(3 + T * (V + pad) + 8, dtype=dtype, device="cuda")
+    many = store.as_strided((T, V), (V + pad, 1), 3)
+    for t in range(0, T, kinds):
+        many[t:t + kinds] = x[:min(kinds, T - t)]
+    target = y[kind].contiguous()
+    off = np.zeros(T, bool)
+    off[r.integers(kinds, T, T // 9)] = True
+    off[T // 2:T // 2 + min(600, T // 3)] = True
+    off = torch.from_numpy(off).cuda()
+    target[off] = -1
+    args = [target] + [torch.from_numpy(v).cuda()[kind].contiguous() for v in (old, adv, ref)]
+    kw = dict(reduction="sum", kl=0.1)
+    res = losses.policy_loss(many, *args, **kw)
+    assert (res["dlogits"][off] == 0).all() and (res["logp"][off] == 0).all()
+    on = torch.nonzero(~off)[:, 0]
+    for rows in on.split(256):
+        k = kind[rows]
+        assert ((res["logp"][rows].double() - torch.from_numpy(logp).cuda()[k]).abs() <= torch.from_numpy(elogp).cuda()[k]).all()
+        assert ((res["dlogits"][rows].double() - want[k]).abs() <= tol[k]).all()
+    # the sums: every kind's terms as often as it occurs
+    times = np.bincount(kind[on].cpu().numpy(), minlength=kinds)
+    total, got = times @ terms, on_host(res["terms"])
+    assert abs(got[0] - total[0]) <= times @ (A * (ratio * er + 4 * U * (ratio + 1)))
+    assert abs(got[1] - total[1]) <= times @ ekl
+    assert got[2] == total[2] and total[2] > 0
+    # other places for the gradient
+    outs = torch.full((2 + T * (V + 1) + 40,), 7.0, dtype=dtype, device="cuda")
+    out = outs.as_strided((T, V), (V + 1, 1), 2)
+    again = losses.policy_loss(many, *args, out=out, **kw)
+    assert torch.equal(out, res["dlogits"]) and all(torch.equal(again[k], res[k]) for k in ("loss", "terms", "logp"))
+    out.fill_(7.0)
+    assert (outs == 7.0).all()
+    alone = losses.policy_loss(many, *args, grad=False, **kw)
+    assert all(torch.equal(alone[k], res[k]) for k in ("loss", "terms", "logp"))
+    losses.policy_loss(many, *args, out=many, **kw)
+    assert torch.equal(many, res["dlogits"])
