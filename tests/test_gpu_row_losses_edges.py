@@ -287,3 +287,18 @@ def test_policy_of_many_rows(cuda, losses, dtype, V, T):
     assert all(torch.equal(alone[k], res[k]) for k in ("loss", "terms", "logp"))
     losses.policy_loss(many, *args, out=many, **kw)
     assert torch.equal(many, res["dlogits"])
+
+
+def test_outputs_keep_nothing_else(cuda, losses):
+    """A loss or a score that is kept, or saved, holds its own bytes and neither the workspace's nor another's."""
+    torch = cuda
+    _, x, y = make(torch, torch.float32, 40, 600)
+    f = torch.zeros(40, device="cuda")
+    off = torch.arange(0, 41, 10, dtype=torch.int32, device="cuda")
+    logp, stats = losses.token_logprob(x, y)
+    outs = [logp, stats, losses.token_logprob_grad(x, y, stats, f)]
+    for res in (losses.preference_loss(x, y, off), losses.balance_loss(x[:, :16], 2),
+                losses.policy_loss(x, y, f, f, f, kl=0.1, offsets=off, reduction="sequences")):
+        outs += res.values()
+    assert all(t.is_contiguous() and t.untyped_storage().nbytes() == t.numel() * t.element_size() for t in outs)
+    assert len({t.untyped_storage().data_ptr() for t in outs}) == len(outs)
