@@ -44,11 +44,12 @@ struct Balance {
   float alpha;
 };
 
-// What bounds it: instruction issue.  65536 tokens x 256 experts, k = 8, fp32:
-// 64 us, of which the choice 37 (comparisons on the ALU) and the gradient 27
-// (205 instructions a token); reading and writing the logits would take 20.  More or
-// fewer than 4 CTAs of 256 threads per SM are slower (with sorted keys 67 us at 60000 x 256; 70
-// with 3, 72 to 76 with 6 and 8).  16384 x 128 bf16: 18 us on the GPU.
+// What bounds it, at 65536 tokens x 256 experts, k = 8, fp32 (64 us, of which the
+// choice 37 and the gradient 27; reading and writing the logits would take 20): the choice the ALU
+// (63 % busy with 417 instructions a token, comparisons mostly) and the latencies between
+// them; the gradient the memory's latency (205 instructions a token are 40 % of the issue slots; 134 MB in 27 us are
+// 4.8 TB/s).  More or fewer than 4 CTAs of 256 threads per SM are slower (60000 x 256: 60 us; 66
+// with 3, 72 with 6, 68 with 8).  16384 x 128 bf16: 18 us on the GPU.
 //
 // A token belongs to L lanes, lane l of them has experts l R .. l R + R - 1 in
 // registers (-inf behind the last expert): as many tokens per warp as fit.
@@ -232,10 +233,10 @@ __device__ __forceinline__ int choose_keys(const float (&v)[R], int l, int k) {
 
 // For a whole warp per token and k <= kFew: the k-th largest of the lanes'
 // maxima is no more than the k-th largest logit, and few logits reach it.  They are gathered, one
-// per lane, and the largest of them (ties: the lowest expert) is taken k times:
-// half the instructions of sorted lanes (60000 x 256 fp32, k = 8: 60 us for the call, 66
+// per lane, and the largest of them (ties: the lowest expert) is taken k times,
+// in fewer instructions than sorted lanes (60000 x 256 fp32, k = 8: 60 us for the call, 67
 // with sorted keys; 30000 x 384 bf16: 56, 60).  bf16 up to 256 experts stays with keys that
-// hold logit and expert at once (51, 56 this way).  -2: more than 32 reach it.
+// hold logit and expert at once (60000 x 256: 50, 56 this way).  -2: more than 32 reach it.
 constexpr int kFew = 8;
 template <int R>
 __device__ __forceinline__ int choose_few(const float (&v)[R], int lane, int k, uint2* slot) {
@@ -434,8 +435,8 @@ __global__ void __launch_bounds__(kSmallThreads) balance_small_kernel(Balance a)
 constexpr int64_t kWorkBytes = (sizeof(Head) + 255) / 256 * 256 + kMaxGrid * sizeof(Sum);
 
 // Tokens times lanes of one: one CTA takes up to two passes of its 1024 threads
-// (5.7 to 8 us for one, 8.3 to 12.6 for two, on the GPU); the two kernels and
-// the clearing before them take 10.3 and two more calls of the driver.
+// (512 x 8, two passes: 20 us a call; 26.5 with the two kernels and the clearing before
+// them; one token of 64 experts: 20 and 25).
 constexpr int64_t kSmallLanes = 2 * kSmallThreads;
 template <typename X, int L, int R>
 cudaError_t launch_balance(Balance a, cudaStream_t st) {

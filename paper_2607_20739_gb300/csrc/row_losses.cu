@@ -908,8 +908,8 @@ int sm_count() {
 // How the rows of a streaming pass lie on the grid: a warp each, a CTA each, or
 // a cluster each.  A warp takes a row up to 24 KB where there are rows for all
 // warps (bf16, 8192 classes, forward and gradient: 115 and 181 us for 800 and
-// 1200 MB, at the copy rate; 164 and 192 with CTAs; at 32 KB the gradient turns: 191
-// and 175), else one up to 4 KB.  Few long rows are split over a cluster while
+// 1200 MB, at the copy rate; 168 and 192 with CTAs; at 32 KB the gradient turns: 193
+// and 175, the forward pass 124 and 130), else one up to 4 KB.  Few long rows are split over a cluster while
 // the SMs hold more CTAs and a part stays above 4 KB.
 constexpr int64_t kWarpRowBytes = 4 * 1024, kWarpManyRowsBytes = 24 * 1024;
 struct Shape {
@@ -957,9 +957,9 @@ cudaError_t launch(void (*kernel)(P...), unsigned grid, int threads, int ranks, 
 bool in_pairs(const pgc_logits* z) { return z->classes % 2 == 0 && z->ld % 2 == 0 && (uintptr_t)z->x % 4 == 0; }
 // Short rows: up to 128 classes by 8 lanes, 256 by 16, 512 by 32 (fp32, and bf16 in
 // pairs); rows above are read in 16-byte pieces by a warp.  131072 rows of 10, 100 and 256 bf16
-// classes: forward 15, 14 and 21 us a call (36, 46 and 50 in pieces), gradient 14, 14
-// and 27 (33, 59 and 62), policy 31, 33 and 54 (85, 89 and 89); 65536 x 511 fp32 gradient 45 (55), x 512
-// bf16 27 (39).  Up to 1024 classes this way the policy loss turns: 74 us for 87040 x 1000 bf16, 64 in pieces.
+// classes: forward 14, 12 and 20 us a call (36, 46 and 50 in pieces), gradient 12, 15
+// and 27 (33, 58 and 62), policy (130624 rows) 28, 33 and 55 (85, 89 and 89); gradient of 65536 x 511 fp32 44 (54) and x 512
+// bf16 27 (39).  Up to 1024 classes this way the policy loss turns: 84 us for 65337 x 1000 bf16, 64 in pieces.
 bool short_rows(const pgc_logits* z) { return z->classes <= (z->dtype == PGC_F32 || in_pairs(z) ? 512 : 256); }
 unsigned short_grid(const pgc_logits* z) {
   const int64_t rows = kWarps * (z->classes <= 128 ? 4 : z->classes <= 256 ? 2 : 1);
@@ -999,8 +999,9 @@ cudaError_t launch_stats(const pgc_logits* z, float* logp, float2* stats, Head* 
                 s.grid, kThreads, s.ranks, false, 0, st, rows_of(z), logp, stats, head);
 }
 
-// The gradient pass takes a row in parts of 32 to 64 KB: smaller grains level
-// the last wave (2000 x 50001 fp32: 115 us, 124 with whole rows; parts of 16 KB 127).
+// The gradient pass takes a row that a CTA or a cluster has in parts of 32 to 64 KB (whole up to 64 KB; few
+// rows in as many parts as the cluster has CTAs, of 4 KB at least): smaller grains
+// level the last wave (2000 x 50001 fp32: 114 us, 125 with whole rows; parts of 16 KB 127).
 constexpr int64_t kGradPartBytes = 32 * 1024;
 cudaError_t launch_grad(const pgc_logits* z, const float* coef, const float2* stats, const Head* head, cudaStream_t st) {
   if (z->rows == 0) return cudaSuccess;
@@ -1018,17 +1019,18 @@ cudaError_t launch_grad(const pgc_logits* z, const float* coef, const float2* st
 
 constexpr int kMaxParts = 1024;       // CTAs of the kernels that leave partial sums
 
-// Policy loss.  Rows up to 12 KB are a warp's (bf16, 4096 classes: 84 us with
-// warps, 104 with CTAs; at 16 KB 117 against 110), longer ones a CTA's: of 128
+// Policy loss.  Rows up to 12 KB are a warp's (bf16, 24041 x 4096: 83 us with
+// warps, 104 with CTAs; 16816 x 8192, 16 KB a row: 116 against 109), longer ones a CTA's: of 128
 // threads up to 36 KB, of 256 up to 110, of 512 above (a thread then has about
 // 16 places, and the SM as many warps as its shared memory allows rows for:
-// 16384 classes 111 us with 128 threads, 121 with 256).  A row between 110 and 148 KB
+// 12195 x 16384: 142 us with 128 threads, 157 with 256).  A row between 110 and 148 KB
 // leaves room for no second one on the SM, so two CTAs of a cluster share it
-// (65536 classes: 217 us, 252 by one CTA); more CTAs per row cost more than
-// they bring, as each waits for the others of its row (100003 classes: 230 us by
-// one CTA, 355 by three), but where rows are too few for the SMs they halve a
-// row's time.  Above 216 KB a row is read twice by 1024 threads (131072
-// classes: 282 us; 338 in two halves held by two SMs).
+// (4506 x 65536: 226 us, 254 by one CTA); beyond that sharing costs more than
+// it brings, as each CTA waits for the other (4472 x 100000: 342 us by one CTA, 351 by two),
+// but where rows are too few for the SMs more CTAs shorten a row's
+// time.  A thread's places are even, so 512 threads hold rows in steps of 16 KB, the longest
+// 208 KB; above that a row is read twice by 1024 threads (4472 x 131072:
+// 446 us, 534 in two halves held by two SMs; 4472 x 100000 read twice: 382).
 constexpr int64_t kHeldWarpBytes = 12 * 1024, kHeld128Bytes = 36 * 1024, kHeld256Bytes = 110 * 1024,
                   kHeldPairBytes = 148 * 1024, kHeldSmem = 216 * 1024;
 // Shared memory above 48 KB is asked for once per device and kernel.
