@@ -1133,11 +1133,14 @@ int pgc_loss_workspace(int64_t rows, int64_t sequences, int64_t *bytes) {
 }
 
 int pgc_token_logprob(const pgc_logits *z, float *logp, float *stats, void *stream) {
-  int rc = check_rows(z, false);
+  if (!z) return PGC_EINVAL;
+  pgc_logits forward = *z;              // z->grad and its pitch are not used
+  forward.grad = nullptr;
+  int rc = check_rows(&forward, false);
   if (rc) return rc;
   if (z->rows && (!logp || !stats)) return PGC_EINVAL;
   if ((uintptr_t)logp % 4 || (uintptr_t)stats % 8) return PGC_EINVAL;
-  return report_cuda(launch_stats(z, logp, reinterpret_cast<float2*>(stats), nullptr, (cudaStream_t)stream));
+  return report_cuda(launch_stats(&forward, logp, reinterpret_cast<float2*>(stats), nullptr, (cudaStream_t)stream));
 }
 
 int pgc_token_logprob_grad(const pgc_logits *z, const float *stats, const float *dlogp, void *stream) {
