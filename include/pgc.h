@@ -408,9 +408,10 @@ int pgc_gradient_noalloc(int32_t loss, int32_t dtype, int64_t m, int64_t d, cons
  *  - A row whose target is negative takes no part (prompts, padding): its logits are
  *    not read, its log probability is 0 and its gradient row is zeros.  A
  *    target >= classes is not followed: log probability, gradient row and
- *    loss are NaN.  A row all of whose logits are -inf has no distribution: NaN
- *    as well.  A target of logit -inf has log probability -inf.  Classes may be masked by -inf
- *    or by any large negative number, down to the type's lowest value.
+ *    loss are NaN (zeros in a gradient row of no sequence, or of derivative 0).  A row
+ *    all of whose logits are -inf has no distribution: NaN as well.  A target of logit
+ *    -inf has log probability -inf.  Classes may be masked by -inf or by any large
+ *    negative number, down to the type's lowest value.
  *  - offsets: int32, sequence i is rows offsets[i] .. offsets[i + 1] - 1 (so
  *    a padded batch is offsets of equal steps, its padding rows of negative
  *    target).  Rows of no sequence take no part.  Offsets that fall or leave [0, rows]

@@ -165,6 +165,14 @@ __global__ void __launch_bounds__(kThreads) row_stats_kernel(Rows a, float* logp
   }
 }
 
+// A row's coefficient: 0 where nothing is asked of it, whatever its target, and
+// NaN where that is no class.
+__device__ __forceinline__ float row_coef(bool bad, int32_t y, int32_t V, const float* coef) {
+  if (bad) return NAN;
+  const float k = y < 0 ? 0.f : *coef;
+  return y >= V && k != 0.f ? NAN : k;
+}
+
 // A row, or one of its `parts`, per group: nothing is exchanged between them.
 template <typename E, int G>
 __global__ void __launch_bounds__(kThreads) row_grad_kernel(Rows a, int parts, const float* coef, const float2* stats,
@@ -179,7 +187,7 @@ __global__ void __launch_bounds__(kThreads) row_grad_kernel(Rows a, int parts, c
   const Slice s = slice_of(x, a.V, rank, ranks);
   if (head) wait_for_previous();
   const bool bad = head && head->bad;
-  const float k = bad || y >= a.V ? NAN : y < 0 ? 0.f : coef[t];
+  const float k = row_coef(bad, y, a.V, coef + t);
   if (k == 0.f || isnan(k)) {
     slice_fill<E, G>(g, s.first, s.last, tid, k);
     return;
@@ -291,7 +299,7 @@ __global__ void __launch_bounds__(kThreads) short_grad_kernel(Rows a, const floa
   short_load<E, L, P>(static_cast<const E*>(a.x) + t * a.ld, l, a.V, y >= 0, v);
   if (head) wait_for_previous();
   const bool bad = head && head->bad;
-  const float k = bad || y >= a.V ? NAN : y < 0 ? 0.f : coef[t];
+  const float k = row_coef(bad, y, a.V, coef + t);
   const float2 st = y >= 0 ? stats[t] : make_float2(0.f, 0.f);
 #pragma unroll
   for (int j = 0; j < R; ++j) v[j] = ex2((v[j] - st.x) * a.c - st.y * kLog2e);

@@ -302,3 +302,23 @@ def test_outputs_keep_nothing_else(cuda, losses):
         outs += res.values()
     assert all(t.is_contiguous() and t.untyped_storage().nbytes() == t.numel() * t.element_size() for t in outs)
     assert len({t.untyped_storage().data_ptr() for t in outs}) == len(outs)
+
+
+@pytest.mark.parametrize("V", [50, 9001, 40000])
+def test_targets_that_are_none_where_nothing_is_asked(cuda, losses, V):
+    """A target that is no class makes the gradients NaN that depend on it; a row outside every sequence, or of
+    derivative 0, takes no part whatever its target."""
+    torch = cuda
+    _, x, y = make(torch, torch.float32, 8, V, seed=6)
+    y[0] = y[5] = y[7] = V
+    off = torch.tensor([1, 3, 5], dtype=torch.int32, device="cuda")
+    res = losses.preference_loss(x, y, off)
+    assert res["loss"].isfinite() and res["dlogits"].isfinite().all() and (res["dlogits"][[0, 5, 6, 7]] == 0).all()
+    f = torch.zeros(8, device="cuda")
+    pol = losses.policy_loss(x, y, f - 5, f + 1, offsets=off, reduction="sequences")
+    assert pol["loss"].isfinite() and (pol["dlogits"][[0, 5, 6, 7]] == 0).all()
+    _, stats = losses.token_logprob(x, y)
+    one = f + 1
+    one[[0, 3]] = 0
+    d = losses.token_logprob_grad(x, y, stats, one)
+    assert (d[[0, 3]] == 0).all() and d[[5, 7]].isnan().all() and d[[1, 2, 4, 6]].isfinite().all()
