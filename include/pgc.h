@@ -519,6 +519,140 @@ int pgc_balance_loss(int32_t dtype, int64_t rows, int64_t experts, const void *l
                      int32_t k, int32_t given, int32_t *choice, float alpha, float *loss, int32_t *counts, void *grad,
                      int64_t grad_ld, void *workspace, int64_t workspace_bytes, void *stream);
 
+/*
+ * pgc_token_scores — what a row says of its classes beside its target.  With
+ * q_v = (x_v - m) / tau - L the log probability of class v and p = exp(q):
+ *   logp      [rows] q_y; NULL exactly if z->target is NULL, when every row takes part
+ *   entropy   [rows] -sum_v p_v q_v (a class of p = 0 adds nothing)
+ *   top       [rows][k] the classes of the k largest logits, largest first, ties to the lower class
+ *   top_logp  [rows][k] their q.  Where fewer than k logits are above -inf: -1 and -inf
+ *   stats     [rows][2] (8-byte aligned) = (m, L), as pgc_token_logprob returns it
+ * A row of negative target: 0, 0, -1, -inf, (0, 0).  A target >= classes: logp alone is
+ * NaN.  A row with NaN among its logits, or a logit of +inf, has logp, entropy and
+ * top_logp NaN; NaN is no alternative.  z->grad is not used.  k may exceed the classes; 0 <= k <= 64,
+ * PGC_ENOTSUP above.
+ */
+int pgc_token_scores(const pgc_logits *z, int32_t k, float *logp, float *entropy, int32_t *top, float *top_logp,
+                     float *stats, void *stream);
+
+/*
+ * pgc_token_scores_grad — the gradient of any loss whose derivatives with respect to the rows' log
+ * probabilities and entropies are dlogp[rows] and dentropy[rows] (either may be NULL, but not both):
+ *   z->grad[t][v] = (dlogp[t] ([v = y_t] - p_tv) - dentropy[t] p_tv (q_tv + H_t)) / tau.
+ * stats, entropy: as pgc_token_scores returned them for the same logits (entropy is read with
+ * dentropy only).  dlogp needs z->target.  A row of negative target, or whose
+ * derivatives are both 0, gets zeros; a target >= classes NaN unless its dlogp is 0; a row without a
+ * distribution, or with a NaN derivative, NaN.
+ */
+int pgc_token_scores_grad(const pgc_logits *z, const float *stats, const float *entropy, const float *dlogp,
+                          const float *dentropy, void *stream);
+
+/* ---- tokens to their experts and back --------------------------------------- */
+
+/*
+ * A router chose k experts for each of `tokens` tokens (as pgc_balance_loss
+ * does): slot s = t k + j holds an expert, or, outside [0, experts), nothing.
+ * pgc_route sorts the slots by expert; the other calls move rows of d elements
+ * (dtype) between the tokens' order and that one, so that the experts'
+ * products are made over consecutive rows: those of expert e are
+ * offsets[e] .. offsets[e + 1] - 1.
+ *
+ * Common to all of them: what is common to the losses on rows of logits.  Also:
+ *  - place [tokens][k]: the row of each slot.  An entry outside [0, rows) has no row: it
+ *    is not copied, adds nothing, and its weight's gradient is 0.  So `rows` may be less
+ *    than the slots that hold an expert (rows behind it are cut off).  Entries that
+ *    have a row differ from one another.
+ *  - Rows of the experts' order that no slot has are left as they were.
+ *  - Sums run over j in order, in 32 bits; a bf16 result is rounded once.
+ *  - rows, tokens < 2^31 and tokens k < 2^31, 1 <= d < 2^31, d <= pitch <= 2^31; k <= 64 and experts <= 1024,
+ *    PGC_ENOTSUP above.  No output overlaps an input, but where it says so.
+ */
+
+/* pgc_route_workspace — bytes of workspace of pgc_route.  Errors: PGC_EINVAL, PGC_ENOTSUP. */
+int pgc_route_workspace(int64_t tokens, int32_t k, int32_t experts, int64_t *bytes);
+
+/*
+ * pgc_route — sorts the slots by expert, in their order within one.
+ *   choice  [tokens][k]
+ *   place   [tokens][k] the row of each slot, -1 where it holds nothing
+ *   slot    [tokens k]  the slot of each row (its token is slot / k), -1 behind the last one
+ *   offsets [experts + 1] the first row of each expert, and their end
+ * A token may hold the same expert twice: two rows.
+ */
+int pgc_route(int64_t tokens, int32_t k, int32_t experts, const int32_t *choice, int32_t *place, int32_t *slot,
+              int32_t *offsets, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* pgc_spread — out[place[t][j]] = x[t].  x: tokens rows of pitch ld; out: `rows` rows of pitch out_ld. */
+int pgc_spread(int32_t dtype, int64_t tokens, int32_t k, int64_t d, const void *x, int64_t ld, const int32_t *place,
+               int64_t rows, void *out, int64_t out_ld, void *stream);
+
+/*
+ * pgc_join — out[t] = sum_j weight[t][j] rows_in[place[t][j]]; weight [tokens][k]
+ * float32, or NULL for ones: the gradient of pgc_spread.  A token without rows gets zeros.
+ */
+int pgc_join(int32_t dtype, int64_t tokens, int32_t k, int64_t d, const void *rows_in, int64_t ld, int64_t rows,
+             const int32_t *place, const float *weight, void *out, int64_t out_ld, void *stream);
+
+/*
+ * pgc_join_grad — the gradient of pgc_join for the derivative dy (tokens rows):
+ *   drows[place[t][j]] = weight[t][j] dy[t],   dweight[t][j] = <dy[t], rows_in[place[t][j]]>.
+ * drows may be rows_in itself (with drows_ld = ld).
+ */
+int pgc_join_grad(int32_t dtype, int64_t tokens, int32_t k, int64_t d, const void *dy, int64_t dy_ld, const void *rows_in,
+                  int64_t ld, int64_t rows, const int32_t *place, const float *weight, void *drows, int64_t drows_ld,
+                  float *dweight, void *stream);
+
+/* ---- AdamW over many tensors ------------------------------------------------- */
+
+/*
+ * pgc_adamw_step — one AdamW step over any number of tensors, in launches of up to
+ * 240 tensors.  With g = grad * grad_scale, every element:
+ *   m' = beta1 m + (1 - beta1) g,   v' = beta2 v + (1 - beta2) g^2,
+ *   p' = p (1 - lr weight_decay) - lr (m' / (1 - beta1^step)) / (sqrt(v' / (1 - beta2^step)) + eps),
+ * in 32 bits; p' is rounded to the parameters' type once, and to bf16 for `copy`.
+ *
+ * bits = 32: m and v are float32.  bits = 8: they are one byte an element, and every 256
+ * elements (a block; the last one of a tensor may be shorter) have two scales, powers of two:
+ *   m : an 8-bit float of 4 bits of exponent (bias 7) and 3 of fraction, times m_scale
+ *   v : code c: 0 for zero; from 127 on 2^(-3 + (c - 127) / 16), below it 2^(-3 + (c - 127) / 8), with
+ *       the fractions of an exponent taken in equal steps (16 or 8 an octave), times v_scale
+ * m_scale is 2^(e - 7) and v_scale 2^(e - 4), 2^e the largest power of two in the block's largest magnitude; a block
+ * whose largest is below 2^-111 becomes zeros.  A value between two codes goes to the
+ * upper one with the probability of its place between them (1 / 65536 steps; a positive v never to 0), by 32
+ * bits drawn from (seed, step, the tensor's index in the list, the element's): the same call
+ * gives the same bits.  The parameters of a step see m' and v' before that rounding.  A block that meets an
+ * infinity or NaN in m' or v' is NaN from then on.  Relative rounding noise that this leaves in v: about 6 %
+ * at beta2 = 0.95 and 40 % at 0.999 (twice that for elements whose v is under 2^-8 of their block's largest).
+ *
+ * Tensors are contiguous and overlap nothing; a NULL grad leaves its tensor as it is.  Moments start as zeros
+ * (all bytes and scales).  The structures are read before the call returns.
+ * Nothing is allocated, the work is ordered on `stream`, and the call returns without waiting.
+ * A captured graph replays the step and lr that it was captured with, but those on the device.
+ * Errors: PGC_EINVAL before any CUDA call (types, bits, NULL, alignment to the element, n outside [0, 2^38],
+ * step < 1, a rate that is not finite, eps < 0, a beta outside [0, 1)), PGC_ECUDA.
+ */
+typedef struct pgc_adamw_tensor {
+  void       *param;          /* [n] param_dtype, updated                          */
+  const void *grad;           /* [n] grad_dtype, or NULL                           */
+  void       *copy;           /* [n] bf16, receives p'; or NULL                    */
+  void       *m, *v;          /* [n] moments                                       */
+  float      *m_scale, *v_scale;  /* bits = 8: [(n + 255) / 256]                   */
+  int64_t     n;
+} pgc_adamw_tensor;
+
+typedef struct pgc_adamw {
+  double lr, beta1, beta2, eps, weight_decay;
+  int64_t step;               /* 1 for the first one                               */
+  const int64_t *step_at;     /* device: in place of step; or NULL                 */
+  const float *lr_at;         /* device: in place of lr; or NULL                   */
+  const float *grad_scale;    /* device: factor of the gradients; or NULL for 1    */
+  uint32_t seed;
+  int32_t param_dtype, grad_dtype;   /* PGC_F32 or PGC_BF16                        */
+  int32_t bits;               /* 32 or 8                                           */
+} pgc_adamw;
+
+int pgc_adamw_step(const pgc_adamw *s, const pgc_adamw_tensor *tensors, int64_t count, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -49,6 +49,18 @@ class Logits(C.Structure):
                 ("temperature", C.c_float)]
 
 
+class AdamWTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("copy", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n", C.c_int64)]
+
+
+class AdamW(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("weight_decay", C.c_double), ("step", C.c_int64), ("step_at", C.c_void_p), ("lr_at", C.c_void_p),
+                ("grad_scale", C.c_void_p), ("seed", C.c_uint32), ("param_dtype", C.c_int32), ("grad_dtype", C.c_int32),
+                ("bits", C.c_int32)]
+
+
 _vp = C.c_void_p
 _i32 = C.c_int32
 _i64 = C.c_int64
@@ -92,6 +104,14 @@ _sig = {
     "pgc_balance_workspace": (C.c_int, [_i64, _i64, C.POINTER(_i64)]),
     "pgc_balance_loss": (C.c_int, [_i32, _i64, _i64, _vp, _i64, _vp, _i32, _i32, _vp, C.c_float, _vp, _vp, _vp, _i64,
                                    _vp, _i64, _vp]),
+    "pgc_token_scores": (C.c_int, [C.POINTER(Logits), _i32, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "pgc_token_scores_grad": (C.c_int, [C.POINTER(Logits), _vp, _vp, _vp, _vp, _vp]),
+    "pgc_route_workspace": (C.c_int, [_i64, _i32, _i32, C.POINTER(_i64)]),
+    "pgc_route": (C.c_int, [_i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "pgc_spread": (C.c_int, [_i32, _i64, _i32, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp]),
+    "pgc_join": (C.c_int, [_i32, _i64, _i32, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _i64, _vp]),
+    "pgc_join_grad": (C.c_int, [_i32, _i64, _i32, _i64, _vp, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _i64, _vp, _vp]),
+    "pgc_adamw_step": (C.c_int, [C.POINTER(AdamW), C.POINTER(AdamWTensor), _i64, _vp]),
 }
 for _name, (_res, _args) in _sig.items():
     _f = getattr(lib, _name)

@@ -19,67 +19,13 @@ Common arguments:
 
 from __future__ import annotations
 
-import ctypes as C
-import functools
-
 import torch
 
 from . import binding as B
+from ._tensors import _TYPES, _address, _bytes, _matrix, _on, _vector
 
-__all__ = ["token_logprob", "token_logprob_grad", "preference_loss", "policy_loss", "balance_loss"]
-
-_TYPES = {torch.float32: B.F32, torch.bfloat16: B.BF16}
-
-# A call on few rows lasts as long as its marshalling: the current stream's
-# handle is asked for directly (torch.cuda.current_stream takes 2 us) and sizes are
-# kept.  Every output has a storage of its own (1.4 us each; a view of a common one 0.9), so
-# that a loss that is kept keeps no workspace.
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
-    (lambda index: torch.cuda.current_stream(index).cuda_stream)
-
-
-def _address(t):
-    return None if t is None else t.data_ptr()
-
-
-def _vector(name, t, dtype, shape, device):
-    """Refuses what is not a contiguous tensor of that type and shape on that device."""
-    try:
-        if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
-            return
-    except AttributeError:
-        pass
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch tensor")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the logits are on {device}")
-    if t.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-    raise ValueError(f"{name} must be contiguous")
-
-
-def _matrix(name, t):
-    """(rows, classes, pitch) of a tensor whose rows are contiguous."""
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch tensor")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor")
-    if t.dim() != 2 or t.dtype not in _TYPES:
-        raise ValueError(f"{name} must be [rows, classes] in float32 or bfloat16")
-    rows, classes = t.shape
-    pitch, step = t.stride()
-    if classes < 1:
-        raise ValueError(f"{name} must have a class")
-    if classes > 1 and step != 1:
-        raise ValueError(f"rows of {name} must be contiguous")
-    if rows < 2:
-        return rows, classes, classes
-    if pitch < classes:
-        raise ValueError(f"rows of {name} overlap")
-    return rows, classes, pitch
-
+__all__ = ["token_logprob", "token_logprob_grad", "token_scores", "token_scores_grad", "preference_loss", "policy_loss",
+           "balance_loss"]
 
 def _gradient(logits, out, grad):
     """The tensor for the gradient and its pitch."""
@@ -94,33 +40,6 @@ def _gradient(logits, out, grad):
     if out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device:
         raise ValueError("out must have the logits' shape, type and device")
     return out, pitch
-
-
-def _on(device, stream, tensors, call):
-    """call(stream handle) with the device and stream current; tensors given
-    are kept from reuse until a stream that is not current is past the call."""
-    if stream is None and device.index == torch.cuda.current_device():
-        return call(_raw_stream(device.index))
-    if stream is None:
-        stream = torch.cuda.current_stream(device)
-    elif not hasattr(stream, "cuda_stream"):
-        stream = torch.cuda.ExternalStream(int(stream), device=device) if int(stream) else \
-            torch.cuda.default_stream(device)
-    if stream.device != device:
-        raise ValueError(f"the stream is on {stream.device}, the logits are on {device}")
-    with torch.cuda.stream(stream):
-        result = call(stream.cuda_stream)
-    for t in tensors:
-        if t is not None:
-            t.record_stream(stream)
-    return result
-
-
-@functools.lru_cache(maxsize=4096)
-def _bytes(query, *sizes):
-    n = C.c_int64()
-    B._check(getattr(B.lib, query)(*sizes, C.byref(n)), query)
-    return n.value
 
 
 def token_logprob(logits, target, temperature=1.0, *, stream=None):
@@ -155,6 +74,62 @@ def token_logprob_grad(logits, target, stats, dlogp, temperature=1.0, *, out=Non
         B._check(B.lib.pgc_token_logprob_grad(z, stats.data_ptr(), dlogp.data_ptr(), st), "pgc_token_logprob_grad")
         return dlogits
     return _on(device, stream, (logits, target, stats, dlogp, out), call)
+
+
+def token_scores(logits, target=None, k=0, temperature=1.0, *, stream=None):
+    """Log probability of every row's target, the row's entropy, and its k likeliest classes.
+
+    Returns a dict: logp (float32 [rows]; None without target, when every row takes part),
+    entropy (float32 [rows]), top (int32 [rows, k], largest first, ties to the lower class; -1
+    where there is none), top_logp (float32 [rows, k], -inf there), stats (float32
+    [rows, 2], which ``token_scores_grad`` and ``token_logprob_grad`` take).
+    """
+    rows, classes, ld = _matrix("logits", logits)
+    device = logits.device
+    if target is not None:
+        _vector("target", target, torch.int32, (rows,), device)
+
+    def call(st):
+        logp = None if target is None else torch.empty(rows, dtype=torch.float32, device=device)
+        entropy = torch.empty(rows, dtype=torch.float32, device=device)
+        top = torch.empty((rows, max(k, 0)), dtype=torch.int32, device=device)
+        top_logp = torch.empty((rows, max(k, 0)), dtype=torch.float32, device=device)
+        stats = torch.empty((rows, 2), dtype=torch.float32, device=device)
+        z = B.Logits(logits.data_ptr(), _address(target), None, rows, classes, ld, 0, _TYPES[logits.dtype], temperature)
+        B._check(B.lib.pgc_token_scores(z, k, _address(logp), entropy.data_ptr(), top.data_ptr(), top_logp.data_ptr(),
+                                        stats.data_ptr(), st), "pgc_token_scores")
+        return {"logp": logp, "entropy": entropy, "top": top, "top_logp": top_logp, "stats": stats}
+    return _on(device, stream, (logits, target), call)
+
+
+def token_scores_grad(logits, target, stats, entropy=None, dlogp=None, dentropy=None, temperature=1.0, *, out=None,
+                      stream=None):
+    """Gradient of the logits for the derivatives dlogp and dentropy (float32 [rows], one of them at
+    least) of a loss with respect to what ``token_scores`` returned: its stats and, with
+    dentropy, its entropy.  target may be None without dlogp."""
+    rows, classes, ld = _matrix("logits", logits)
+    device = logits.device
+    _vector("stats", stats, torch.float32, (rows, 2), device)
+    if dlogp is None and dentropy is None:
+        raise ValueError("dlogp or dentropy must be given")
+    if dlogp is not None and target is None:
+        raise ValueError("dlogp needs target")
+    if dentropy is not None and entropy is None:
+        raise ValueError("dentropy needs entropy")
+    if target is not None:
+        _vector("target", target, torch.int32, (rows,), device)
+    for name, t in (("entropy", entropy), ("dlogp", dlogp), ("dentropy", dentropy)):
+        if t is not None:
+            _vector(name, t, torch.float32, (rows,), device)
+
+    def call(st):
+        dlogits, ldg = _gradient(logits, out, True)
+        z = B.Logits(logits.data_ptr(), _address(target), dlogits.data_ptr(), rows, classes, ld, ldg,
+                     _TYPES[logits.dtype], temperature)
+        B._check(B.lib.pgc_token_scores_grad(z, stats.data_ptr(), _address(entropy), _address(dlogp), _address(dentropy),
+                                             st), "pgc_token_scores_grad")
+        return dlogits
+    return _on(device, stream, (logits, target, stats, entropy, dlogp, dentropy, out), call)
 
 
 def preference_loss(logits, target, offsets, ref_logp=None, *, beta=0.1, kind="sigmoid", margin=0.0, smoothing=0.0,

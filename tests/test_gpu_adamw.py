@@ -1,0 +1,332 @@
+"""AdamW over many tensors against the 64-bit oracle.
+
+u = 2^-24, h half a step of the parameters' type.  m' is rounded three times: em = u (2 |beta1 m| + 2 |(1 - beta1) g| +
+|m'|) with g's own rounding; v' the same, all of its terms positive: 7 u of it
+(g's rounding twice, the square, 1 - beta2, the product, the sum).  The step lr m^ / (sqrt(v^) + eps):
+half of v's error, 2 u each for the root, the sum, the quotient, two products and the three host constants: 20 u of its size, and
+em over m'; the parameter two roundings more, then h.  Moments in 8 bits are equal to the bit."""
+
+import numpy as np
+import pytest
+
+from oracle import training_oracle as O
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+SIZES = [0, 1, 2, 3, 7, 31, 255, 256, 257, 511, 1000, 2047, 2048, 2049, 4099, 70001]
+
+
+@pytest.fixture(scope="module")
+def optim(cuda):
+    from paper_2607_20739_gb300 import optim
+    return optim
+
+
+def on_host(x):
+    return x.double().cpu().numpy()
+
+
+def place(torch, a, dtype, shift):
+    """A copy of `a` that starts `shift` elements into its storage, with 7 around it."""
+    store = torch.full((shift + len(a) + 5,), 7.0, device="cuda").to(dtype)
+    t = store[shift:shift + len(a)]
+    t.copy_(torch.from_numpy(np.asarray(a, np.float32)).to(dtype) if dtype.is_floating_point else torch.from_numpy(a))
+    return t
+
+
+def make(torch, sizes, ptype, gtype, shift=0, seed=0):
+    r = np.random.default_rng([seed, len(sizes)])
+    params, grads = [], []
+    for n in sizes:
+        params.append(place(torch, r.standard_normal(n) * 0.05, ptype, shift))
+        grads.append(place(torch, r.standard_normal(n) * np.exp(r.standard_normal(n)) * 1e-3, gtype, shift))
+    return r, params, grads
+
+
+def check_param(torch, got, want, p, m1, g, step, dtype, lr, betas, decay, m, eps_m):
+    h = torch.finfo(dtype).eps / 2
+    size = np.abs(step)
+    with np.errstate(all="ignore"):
+        rel = np.where(m1 != 0, eps_m / np.abs(m1), 0.0)
+    tol = size * (20 * U + rel) + 4 * U * np.abs(p)
+    tol = tol * (1 + h) + h * np.abs(want) + (1e-40 if h == U else 0.0)
+    err = np.abs(got - want)
+    assert (err <= tol).all(), (np.argwhere(err > tol)[:3], (err / np.maximum(tol, 1e-300)).max())
+
+
+def expected(p, g, m, v, t, lr, betas, eps, decay):
+    q, m1, v1 = O.adamw(p, g, m, v, t, lr, betas, eps, decay)
+    step = p * (1 - lr * decay) - q
+    eps_m = U * (2 * np.abs(betas[0] * m) + 3 * np.abs((1 - betas[0]) * g) + np.abs(m1))
+    return q, m1, v1, step, eps_m
+
+
+@pytest.mark.parametrize("ptype,gtype", [("float32", "float32"), ("float32", "bfloat16"), ("bfloat16", "bfloat16"), ("bfloat16", "float32")])
+@pytest.mark.parametrize("shift", [0, 1, 2, 3, 4])
+@pytest.mark.parametrize("copies", [False, True])
+def test_32_bits(cuda, optim, ptype, gtype, shift, copies):
+    torch = cuda
+    ptype, gtype = getattr(torch, ptype), getattr(torch, gtype)
+    lr, betas, eps, decay = 3e-3, (0.9, 0.99), 1e-8, 0.1
+    r, params, grads = make(torch, SIZES, ptype, gtype, shift)
+    halves = [place(torch, np.zeros(n), torch.bfloat16, shift) for n in SIZES] if copies else None
+    state = None
+    if shift:
+        state = {"t": 0, "m": [place(torch, np.zeros(n), torch.float32, shift % 4) for n in SIZES],
+                 "v": [place(torch, np.zeros(n), torch.float32, (2 * shift) % 4) for n in SIZES]}
+    opt = optim.AdamW(params, lr=lr, betas=betas, eps=eps, weight_decay=decay, copies=halves, state=state)
+    for t in range(1, 4):
+        before = [(on_host(p), on_host(m), on_host(v)) for p, m, v in zip(params, opt.m, opt.v)]
+        scale = torch.tensor(0.37, device="cuda") if t == 3 else None
+        opt.step(grads, grad_scale=scale)
+        assert opt.t == t
+        for i, (p, m, v) in enumerate(before):
+            g = on_host(grads[i]) * (1.0 if scale is None else float(scale))
+            q, m1, v1, step, em = expected(p, g, m, v, t, lr, betas, eps, decay)
+            assert (np.abs(on_host(opt.m[i]) - m1) <= em + 1e-44).all()
+            assert (np.abs(on_host(opt.v[i]) - v1) <= 7 * U * v1 + 1e-44).all()
+            check_param(torch, on_host(params[i]), q, p, m1, g, step, ptype, lr, betas, decay, m, em)
+            if copies:
+                check_param(torch, on_host(halves[i]), q, p, m1, g, step, torch.bfloat16, lr, betas, decay, m, em)
+    for group in (params, opt.m, opt.v) + ((halves,) if copies else ()):
+        for x in group:
+            if x.storage_offset() or group is params:
+                around = torch.empty(0, dtype=x.dtype, device="cuda").set_(x.untyped_storage())
+                assert (around[:x.storage_offset()].float() == 7).all()
+                assert (around[x.storage_offset() + x.numel():].float() == 7).all()
+
+
+@pytest.mark.parametrize("ptype,gtype", [("float32", "float32"), ("float32", "bfloat16"), ("bfloat16", "bfloat16"), ("bfloat16", "float32")])
+@pytest.mark.parametrize("shift", [0, 1, 4, 8])
+@pytest.mark.parametrize("copies", [False, True])
+def test_8_bits(cuda, optim, ptype, gtype, shift, copies):
+    torch = cuda
+    ptype, gtype = getattr(torch, ptype), getattr(torch, gtype)
+    kw = dict(lr=3e-3, eps=1e-8)
+    betas, decay, seed = (0.9, 0.95), 0.1, 12345
+    r, params, grads = make(torch, SIZES, ptype, gtype, shift)
+    halves = [place(torch, np.zeros(n), torch.bfloat16, shift) for n in SIZES] if copies else None
+    state = None
+    if shift:
+        blocks = [-(-n // 256) for n in SIZES]
+        state = {"t": 0, "m": [torch.zeros(shift + n, dtype=torch.uint8, device="cuda")[shift:].view(torch.float8_e4m3fn) for n in SIZES],
+                 "v": [torch.zeros(shift + n, dtype=torch.uint8, device="cuda")[shift:] for n in SIZES],
+                 "m_scale": [torch.zeros(n + 1, device="cuda")[1:] for n in blocks],
+                 "v_scale": [torch.zeros(n + 1, device="cuda")[1:] for n in blocks]}
+    opt = optim.AdamW(params, betas=betas, weight_decay=decay, bits=8, copies=halves, seed=seed, state=state, **kw)
+    codes = lambda x: x.view(torch.uint8).cpu().numpy()  # noqa: E731
+    for t in range(1, 5):
+        before = [(on_host(p), codes(m), codes(v), a.cpu().numpy(), b.cpu().numpy())
+                  for p, m, v, a, b in zip(params, opt.m, opt.v, opt.m_scale, opt.v_scale)]
+        scale = torch.tensor(0.37, device="cuda") if t == 3 else None
+        if t == 4:                                   # a step of other gradients: blocks of zeros, and of few elements
+            grads = [torch.where(torch.arange(g.numel(), device="cuda") % 600 < 300, g, g * 0) for g in grads]
+        opt.step(grads, grad_scale=scale)
+        for i, (p, m, v, a, b) in enumerate(before):
+            if not len(p):
+                continue
+            g = on_host(grads[i]).astype(np.float32)
+            q, mc, vc, ms, vs = O.adamw8(p, g, m, v, a, b, t, i, seed, betas, None if scale is None else float(scale), decay=decay, **kw)
+            assert (opt.m_scale[i].cpu().numpy() == ms).all() and (opt.v_scale[i].cpu().numpy() == vs).all()
+            assert (codes(opt.m[i]) == mc).all()
+            assert (codes(opt.v[i]) == vc).all()
+            at = np.arange(len(p)) // 256
+            mv, vv = O.decode_m(m) * a[at], O.decode_v(v) * b[at]
+            g64 = g.astype(np.float64) * (1.0 if scale is None else float(scale))
+            q, m1, v1, step, em = expected(p, g64, mv, vv, t, 3e-3, betas, 1e-8, decay)
+            check_param(torch, on_host(params[i]), q, p, m1, g64, step, ptype, 3e-3, betas, decay, mv, em)
+            if copies:
+                check_param(torch, on_host(halves[i]), q, p, m1, g64, step, torch.bfloat16, 3e-3, betas, decay, mv, em)
+
+
+def test_8_bits_follow_32(cuda, optim):
+    """Two hundred steps of gradients of their own sizes, 2^-6 to 2^6 apart in a block: the moments stay those of 32 bits within
+    their rounding noise.  v: a rounding of relative variance at most (step / 2)^2, a step 1 / 16 of a value (1 / 8 where it
+    is below 2^-8 of its block's largest), kept by 1 / (1 - beta2^2): at beta2 = 0.9 a standard deviation of 0.07 (0.14); the mean over
+    2^14 elements is within 6 / 2^7 of that, whatever the tails."""
+    torch = cuda
+    n, betas = 1 << 16, (0.9, 0.9)
+    r = np.random.default_rng(5)
+    size = torch.from_numpy(2.0 ** r.integers(-6, 7, n)).float().cuda()
+    p = torch.zeros(n, device="cuda")
+    p2 = torch.zeros(n, device="cuda")
+    a, b = optim.AdamW([p], betas=betas, bits=8, seed=3), optim.AdamW([p2], betas=betas)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    for _ in range(200):
+        g = torch.randn(n, generator=gen, device="cuda") * size
+        a.step([g])
+        b.step([g])
+    v = torch.from_numpy(O.decode_v(a.v[0].cpu().numpy())).cuda() * a.v_scale[0].double().repeat_interleave(256)
+    ratio = (v / b.v[0].double())
+    for lo, hi, noise in ((2.0 ** -1, 2.0 ** 7, 0.14), (2.0 ** -6, 2.0 ** -1, 0.14)):
+        on = (size >= lo) & (size < hi)
+        # 2^-6 beside 2^6: v is 2^-24 of the largest, and kept above the lowest code
+        if lo < 0.5:
+            on &= size >= 2.0 ** -3
+        assert abs(float(ratio[on].mean()) - 1) < 6 * noise / np.sqrt(float(on.sum())) + 0.01
+    m = a.m[0].float() * a.m_scale[0].repeat_interleave(256)
+    assert float((m - b.m[0]).norm() / b.m[0].norm()) < 0.125 / 2 / np.sqrt(1 - 0.81) + 0.01
+    assert float((p - p2).abs().max()) < 0.5 * 200 * 1e-3
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_none_many_and_zero(cuda, optim, bits):
+    """More tensors than a launch takes, some without a gradient; parameters that never had one stay."""
+    torch = cuda
+    r = np.random.default_rng(0)
+    params = [torch.from_numpy(r.standard_normal(r.integers(1, 600)).astype(np.float32)).cuda() for _ in range(700)]
+    grads = [None if i % 7 == 3 else torch.from_numpy(r.standard_normal(p.numel()).astype(np.float32)).cuda() for i, p in enumerate(params)]
+    old = [p.clone() for p in params]
+    opt = optim.AdamW(params, lr=0.01, weight_decay=0.0, bits=bits)
+    versions = [p._version for p in params]
+    opt.step(grads)
+    for p, q, g in zip(params, old, grads):
+        if g is None:
+            assert torch.equal(p, q)
+        else:
+            # a first step is lr against the gradient's sign (eps 1e-8)
+            want = q.double() - 0.01 * g.double() / (g.double().abs() + 1e-8)
+            assert ((p.double() - want).abs() <= 40 * U * (0.01 + q.double().abs())).all()
+    assert all(p._version > v for p, v in zip(params, versions))
+    zero = torch.zeros(1000, device="cuda")
+    opt = optim.AdamW([zero], bits=bits)
+    opt.step([zero.clone()])
+    assert (zero == 0).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_infinities(cuda, optim, bits):
+    torch = cuda
+    p, g = torch.ones(1000, device="cuda"), torch.ones(1000, device="cuda")
+    g[300] = float("nan")
+    opt = optim.AdamW([p], bits=bits)
+    opt.step([g])
+    assert torch.isnan(p[300]) and torch.isfinite(p).sum() == 999
+    g[300] = 1.0
+    opt.step([g])
+    lost = torch.isnan(p)
+    if bits == 8:
+        assert lost[256:512].all() and lost.sum() == 256        # its block
+    else:
+        assert lost.sum() == 1
+    p, g = torch.ones(1000, device="cuda"), torch.full((1000,), 1e-30, device="cuda")
+    opt = optim.AdamW([p], bits=bits, weight_decay=0.0)         # squares below the smallest float
+    opt.step([g])
+    opt.step([g])
+    assert torch.isfinite(p).all() and ((p - 1).abs() <= 2e-3 + U).all()
+
+
+def test_rates_on_the_device(cuda, optim):
+    """lr and the step's number read by the kernel: captured once, replayed with others, as eager steps."""
+    torch = cuda
+    r, params, grads = make(torch, [5, 300, 4100], torch.float32, torch.bfloat16)
+    for bits in (32, 8):
+        one, two = ([p.clone() for p in params] for _ in range(2))
+        lr = torch.full((), 0.01, device="cuda")
+        a = optim.AdamW(one, lr=lr, bits=bits, seed=9, device_step=True)
+        b = optim.AdamW(two, lr=0.01, bits=bits, seed=9)
+        a.step(grads)
+        b.step(grads)
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            a.step(grads)
+        for t in range(2, 6):
+            lr.fill_(0.01 / t)
+            graph.replay()
+            b.lr = 0.01 / t
+            b.step(grads)
+        torch.cuda.synchronize()
+        assert a.t == b.t == 5
+        for p, q in zip(one, two):
+            # bias corrections by expm1 in single precision: a few u of a step of at most 0.01
+            assert ((p.double() - q.double()).abs() <= 5 * (0.01 * 40 * U + 8 * U * q.double().abs())).all()
+        for x, y in zip(a.m + a.v, b.m + b.v):
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+def test_streams(cuda, optim):
+    torch = cuda
+    r, params, grads = make(torch, [1000, 70000], torch.float32, torch.float32)
+    other = [p.clone() for p in params]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    a, b = optim.AdamW(params), optim.AdamW(other)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        a.step(grads, stream=side)
+        b.step(grads)
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(params, other))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_state_goes_on(cuda, optim, bits):
+    """A state handed on takes the same steps."""
+    torch = cuda
+    r, params, grads = make(torch, [1000, 257], torch.float32, torch.float32)
+    other = [p.clone() for p in params]
+    a = optim.AdamW(params, bits=bits, seed=4)
+    b = optim.AdamW(other, bits=bits, seed=4)
+    for _ in range(2):
+        a.step(grads)
+        b.step(grads)
+    s = b.state()
+    s = {"t": s["t"], **{k: [t.clone() for t in v] for k, v in s.items() if k != "t"}}
+    c = optim.AdamW(other, bits=bits, seed=4, state=s)
+    a.step(grads)
+    c.step(grads)
+    assert c.t == 3 and all(torch.equal(p, q) for p, q in zip(params, other))
+
+
+def test_refusals(cuda, optim):
+    torch = cuda
+    p, q = torch.zeros(10, device="cuda"), torch.zeros(4, 5, device="cuda")
+    for call in (lambda: optim.AdamW([p, q.bfloat16()]), lambda: optim.AdamW([q.t()]), lambda: optim.AdamW([p.half()]),
+                 lambda: optim.AdamW([p, p]), lambda: optim.AdamW([p, p[4:]]), lambda: optim.AdamW([p], copies=[p]),
+                 lambda: optim.AdamW([p], copies=[]), lambda: optim.AdamW([p], copies=[q.bfloat16()]),
+                 lambda: optim.AdamW([p], state={"t": 0, "m": [p], "v": [q.view(-1)[:10]]}),
+                 lambda: optim.AdamW([p], state={"t": -1, "m": [torch.zeros_like(p)], "v": [torch.zeros_like(p)]}),
+                 lambda: optim.AdamW([p], bits=8, state={"t": 0, "m": [torch.zeros_like(p)], "v": [torch.zeros_like(p)]})):
+        with pytest.raises(ValueError):
+            call()
+    opt = optim.AdamW([p, q])
+    for grads in ([p], [p, p], [p, q.t()], [p, q.double()], [p, q.bfloat16()], [p.half(), q.half()], [p.cpu(), q]):
+        with pytest.raises(ValueError):
+            opt.step(grads)
+    for kw in (dict(grad_scale=torch.zeros(2, device="cuda")), dict(grad_scale=torch.zeros((), dtype=torch.float64, device="cuda")),
+               dict(grad_scale=torch.zeros(()))):
+        with pytest.raises(ValueError):
+            opt.step([p, q], **kw)
+    from paper_2607_20739_gb300 import PGCError
+    opt.lr = float("nan")
+    with pytest.raises(PGCError):
+        opt.step([p, q])
+    assert opt.t == 0 and (p == 0).all()
+
+
+def test_elements_beyond_32_bits(cuda, optim):
+    """One tensor of more than 2^32 elements: the last blocks, and those on either side of 2^32."""
+    torch = cuda
+    n = (1 << 32) + 777
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    p = torch.full((n,), 0.5, dtype=torch.bfloat16, device="cuda")
+    g = torch.full((n,), 0.001, dtype=torch.bfloat16, device="cuda")
+    spots = [0, (1 << 31) - 256, 1 << 31, (1 << 32) - 256, 1 << 32, (1 << 32) + 512]
+    for s in spots:
+        g[s:s + 256] = torch.randn(min(256, n - s), device="cuda").bfloat16() * 0.01
+    opt = optim.AdamW([p], bits=8, seed=77, lr=0.01)
+    opt.step([g])
+    for s in spots:
+        e = min(n, s + 256)
+        gs = on_host(g[s:e]).astype(np.float32)
+        zeros = np.zeros(e - s, np.uint8)
+        q, mc, vc, ms, vs = O.adamw8(np.full(e - s, 0.5), gs, zeros, zeros, np.zeros(1, np.float32), np.zeros(1, np.float32), 1, 0, 77,
+                                     (0.9, 0.999), index=s, lr=0.01)
+        assert (opt.m[0][s:e].view(torch.uint8).cpu().numpy() == mc).all()
+        assert (opt.v[0][s:e].cpu().numpy() == vc).all()
+        assert (np.abs(on_host(p[s:e]) - q) <= 2.0 ** -8 * np.abs(q) + 1e-6).all()
+    del p, g, opt
+    torch.cuda.empty_cache()
