@@ -17,8 +17,13 @@
 namespace pgc {
 namespace {
 
-constexpr int kThreads = 256;
+using Key = unsigned long long;
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kUnroll = 4;            // 16-byte pieces a thread has in flight
+constexpr int kMaxCluster = 8;
 constexpr int kMostTop = 64;
+constexpr int kWarpTop = 16;          // alternatives of a row that a warp has
 
 struct Scores {
   const void* x;
@@ -26,117 +31,559 @@ struct Scores {
   const int32_t* y;           // NULL: every row takes part, without a target
   int64_t T, ld, ldg;
   int32_t V, k;
-  float inv_tau;
+  float inv_tau, c;           // 1 / tau, log2(e) / tau
   float *logp, *entropy, *top_logp;
   int32_t* top;
   float2* stats;
 };
 
-__device__ float block_max(float v, float* red) {
-  v = warp_max(v);
-  __syncthreads();
-  if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = v;
-  __syncthreads();
-  v = -INFINITY;
-  for (int i = 0; i < kThreads / 32; ++i) v = fmaxf(v, red[i]);
-  return v;
-}
-__device__ float block_add(float v, float* red) {
-  v = warp_sum(v);
-  __syncthreads();
-  if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = v;
-  __syncthreads();
-  v = 0.f;
-  for (int i = 0; i < kThreads / 32; ++i) v += red[i];
-  return v;
-}
+// ---- sums ------------------------------------------------------------------------
+// Exponents are base 2 and relative to M = fl(m c), as in row_slice.cuh, with
+// w = sum of 2^z z beside s = sum of 2^z: H = ln 2 (log2 s - w / s) whatever M is.
 
-// What is left of e z where e has run out: masked classes have z = -inf.
+struct Part {
+  float m = -INFINITY, M = -kFar, s = 0.f, w = 0.f;
+};
+__device__ __forceinline__ void raise(Part& o, float top, float c) {
+  if (top > o.m) {
+    const float M = ref_of(top, c), d = o.M - M, f = ex2(d);
+    o.w = f * fmaf(d, o.s, o.w);
+    o.s *= f;
+    o.m = top;
+    o.M = M;
+  }
+}
+// 2^z z where 2^z has run out: masked classes have z = -inf.
 __device__ __forceinline__ float times_log(float e, float z) { return e * fmaxf(z, -1e4f); }
-
-// One CTA per row: the maximum, the sums, then the k best one after another.
+__device__ __forceinline__ void add_one(Part& o, float f, float c) {
+  raise(o, f, c);
+  const float z = fmaf(f, c, -o.M), e = ex2(z);
+  o.s += e;
+  o.w += times_log(e, z);
+}
+// A piece with -inf as -2^100 (NaN stays NaN), so that 2^z z is 0 there and not NaN: one instruction for
+// two bf16.  An element below -2^100 adds nothing in a row that is not `extreme` (kSmallC).
 template <typename E>
-__global__ void __launch_bounds__(kThreads) scores_kernel(Scores a) {
-  __shared__ float red[kThreads / 32];
-  __shared__ unsigned long long best;
-  const int64_t t = blockIdx.x;
-  const int tid = threadIdx.x;
-  const int32_t y = a.y ? a.y[t] : 0;
-  int32_t* top = a.top + t * a.k;
-  float* top_logp = a.top_logp + t * a.k;
-  if (y < 0) {
-    for (int j = tid; j < a.k; j += kThreads) {
-      top[j] = -1;
-      top_logp[j] = -INFINITY;
+__device__ __forceinline__ uint4 above(uint4 v);
+template <>
+__device__ __forceinline__ uint4 above<__nv_bfloat16>(uint4 v) {
+  auto at_least = [](uint32_t w) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0xf180f180u));
+    return r;
+  };
+  return make_uint4(at_least(v.x), at_least(v.y), at_least(v.z), at_least(v.w));
+}
+template <>
+__device__ __forceinline__ uint4 above<float>(uint4 v) {
+  auto at_least = [](uint32_t w) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(w)), "f"(-0x1p100f));
+    return __float_as_uint(r);
+  };
+  return make_uint4(at_least(v.x), at_least(v.y), at_least(v.z), at_least(v.w));
+}
+template <typename E, int U>
+__device__ __forceinline__ void add_pieces(Part& o, const uint4 (&v)[U], float c) {
+  constexpr int H = Elem<E>::N / 2;
+  raise(o, Elem<E>::top(v), c);
+  const Pair c2 = pair(c, c), M2 = pair(-o.M, -o.M);
+  Pair sum[2] = {0, 0}, log[2] = {0, 0};
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    Pair f[H];
+    Elem<E>::widen(above<E>(v[u]), f);
+#pragma unroll
+    for (int i = 0; i < H; ++i) {
+      const Pair z = fma2(f[i], c2, M2), e = ex2_2(z);
+      sum[i % 2] = add2(sum[i % 2], e);
+      log[i % 2] = fma2(e, z, log[i % 2]);
     }
-    if (tid == 0) {
-      if (a.logp) a.logp[t] = 0.f;
-      a.entropy[t] = 0.f;
-      a.stats[t] = make_float2(0.f, 0.f);
+  }
+  float lo, hi;
+  split(add2(sum[0], sum[1]), lo, hi);
+  o.s += lo + hi;
+  split(add2(log[0], log[1]), lo, hi);
+  o.w += lo + hi;
+}
+template <typename E, int G>
+__device__ __forceinline__ Part slice_part(const E* x, const Slice& s, int tid, float c) {
+  constexpr int N = Elem<E>::N;
+  Part o;
+  const int body = s.first + s.head, rest = body + s.pieces * N;
+  if (tid < s.head + (s.last - rest)) add_one(o, Elem<E>::get(x + (tid < s.head ? s.first + tid : rest + tid - s.head)), c);
+  const uint4* p = reinterpret_cast<const uint4*>(x + body);
+  for (int i = tid; i < s.pieces; i += G * kUnroll) {
+    uint4 v[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) v[u] = i + u * G < s.pieces ? load16(p + i + u * G) : no_piece(Elem<E>::kLowest);
+    add_pieces<E>(o, v, c);
+  }
+  return o;
+}
+__device__ __forceinline__ Part warp_merge(const Part& o, float c) {
+  Part r;
+  r.m = warp_max(o.m);
+  r.M = ref_of(r.m, c);
+  const float d = o.M - r.M, f = ex2(d);
+  r.s = warp_sum(o.s * f);
+  r.w = warp_sum(f * fmaf(d, o.s, o.w));
+  return r;
+}
+// The same relative to m itself: how CTAs' parts of a row are joined, whatever their M.
+__device__ __forceinline__ float3 at_m(const Part& o, float c) {
+  const float r = fmaf(o.m, c, -o.M), f = ex2(-r);
+  return make_float3(o.m, o.s * f, f * fmaf(-r, o.s, o.w));
+}
+
+template <int G>
+__device__ __forceinline__ void sync_group() {
+  if (G == 32) __syncwarp();
+  else __syncthreads();
+}
+
+// ---- the k largest ---------------------------------------------------------------
+// Every thread knows the largest of its elements.  The k-th largest of these, t, is
+// at most the k-th largest element, so only threads that have met t or more, about k of
+// them, hold alternatives: their pieces are read again (from the L2 cache, as a rule) and
+// what reaches t, a few more than k elements, is ranked.  Keys order by value and then
+// by the lower class; no two are equal.
+
+__device__ __forceinline__ Key key_of(float f, unsigned v) {
+  const uint32_t b = __float_as_uint(f + 0.f);              // zeros of both signs are equal
+  return (Key)(b ^ ((int32_t)b < 0 ? 0xffffffffu : 0x80000000u)) << 32 | (0xffffffffu - v);
+}
+__device__ __forceinline__ int class_of(Key q) { return (int)(0xffffffffu - (uint32_t)q); }
+__device__ __forceinline__ float value_of(Key q) {
+  const uint32_t b = (uint32_t)(q >> 32);
+  return __uint_as_float(b ^ (b & 0x80000000u ? 0x80000000u : 0xffffffffu));
+}
+
+template <int G>
+struct Top {
+  static constexpr int kKeys = G * 8 + kMostTop;            // the ones kept and a step of eight each
+  static constexpr int kTop = G == 32 ? kWarpTop : kMostTop;
+  Key key[kKeys];
+  Key best[kTop];                                           // largest first, 0 where there is none
+  alignas(16) float most[G];
+  uint16_t hot[G];
+  Key red[G / 32];
+  float bound;
+  int keys, hots;
+};
+
+// The k largest of sh.key[0 .. n) into sh.best, by all threads of the group.
+template <int G>
+__device__ __forceinline__ void rank_keys(Top<G>& sh, int n, int k, int tid) {
+  if (tid < k) sh.best[tid] = 0;
+  sync_group<G>();
+  if (n <= 2 * G) {
+    for (int i = tid; i < n; i += G) {
+      const Key mine = sh.key[i];
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += sh.key[j] > mine;
+      if (rank < k) sh.best[rank] = mine;
     }
+    sync_group<G>();
     return;
   }
+  Key before = ~0ull;
+  for (int j = 0; j < k; ++j) {
+    Key most = 0;
+    for (int i = tid; i < n; i += G) {
+      const Key q = sh.key[i];
+      if (q < before && q > most) most = q;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const Key q = __shfl_xor_sync(0xffffffffu, most, o);
+      most = q > most ? q : most;
+    }
+    if (G > 32) {
+      __syncthreads();
+      if (tid % 32 == 0) sh.red[tid / 32] = most;
+      __syncthreads();
+      for (int i = 0; i < G / 32; ++i) most = sh.red[i] > most ? sh.red[i] : most;
+    }
+    before = most;
+    if (tid == 0) sh.best[j] = most;
+    if (most == 0) break;
+  }
+  sync_group<G>();
+}
+template <typename E>
+__device__ __forceinline__ void each(const uint4& v, float (&f)[8]) {
+  Pair h[4];
+  Elem<E>::widen(v, h);
+#pragma unroll
+  for (int i = 0; i < Elem<E>::N / 2; ++i) split(h[i], f[2 * i], f[2 * i + 1]);
+}
+// A slice's pieces in steps of one a thread, keeping the k largest so far: for rows
+// where more elements reach the bound than there are places, mostly classes that are
+// masked by a number, fewer than k others left.
+template <typename E, int G>
+__device__ __noinline__ void top_in_steps(const E* x, Slice s, int tid, int k, Top<G>& sh) {
+  constexpr int N = Elem<E>::N;
+  const int body = s.first + s.head, rest = body + s.pieces * N;
+  Key least = 0;                                             // a key has to be larger
+  int n = 0;
+  sync_group<G>();
+  if (tid == 0) sh.keys = 0;
+  sync_group<G>();
+  auto push = [&](float f, int v) {
+    if (!(f > -INFINITY)) return;
+    const Key q = key_of(f, (unsigned)v);
+    if (q > least) sh.key[atomicAdd(&sh.keys, 1)] = q;
+  };
+  for (int i0 = -G; i0 < s.pieces; i0 += G) {
+    if (i0 < 0) {
+      if (tid < s.head + (s.last - rest)) {
+        const int v = tid < s.head ? s.first + tid : rest + tid - s.head;
+        push(Elem<E>::get(x + v), v);
+      }
+    } else if (i0 + tid < s.pieces) {
+      float f[8];
+      each<E>(load16(reinterpret_cast<const uint4*>(x + body) + i0 + tid), f);
+#pragma unroll
+      for (int j = 0; j < N; ++j) push(f[j], body + (i0 + tid) * N + j);
+    }
+    sync_group<G>();
+    n = sh.keys;
+    if (n > kMostTop) {
+      rank_keys<G>(sh, n, k, tid);
+      n = 0;
+      for (int j = 0; j < k; ++j) n += sh.best[j] != 0;
+      if (n == k) least = sh.best[k - 1];
+      sync_group<G>();
+      if (tid < n) sh.key[tid] = sh.best[tid];
+      if (tid == 0) sh.keys = n;
+    }
+    sync_group<G>();
+  }
+  rank_keys<G>(sh, n, k, tid);
+}
+
+// most: the thread's largest element.
+template <typename E, int G>
+__device__ __forceinline__ void slice_top(const E* x, const Slice& s, int tid, int k, float most, Top<G>& sh) {
+  constexpr int N = Elem<E>::N;
+  sh.most[tid] = most;
+  if (tid == 0) sh.keys = sh.hots = 0;
+  sync_group<G>();
+  int rank = 0;
+#pragma unroll 8
+  for (int i = 0; i < G; i += 4) {
+    const float4 o = *reinterpret_cast<const float4*>(sh.most + i);
+    rank += (o.x > most || (o.x == most && i < tid)) + (o.y > most || (o.y == most && i + 1 < tid)) +
+            (o.z > most || (o.z == most && i + 2 < tid)) + (o.w > most || (o.w == most && i + 3 < tid));
+  }
+  if (rank == k - 1) sh.bound = most;
+  sync_group<G>();
+  const float bound = sh.bound;
+  auto push = [&](float f, int v) {
+    if (!(f >= bound && f > -INFINITY)) return;
+    const int at = atomicAdd(&sh.keys, 1);
+    if (at < Top<G>::kKeys) sh.key[at] = key_of(f, (unsigned)v);
+  };
+  const int body = s.first + s.head, rest = body + s.pieces * N;
+  if (most >= bound && most > -INFINITY) {
+    sh.hot[atomicAdd(&sh.hots, 1)] = (uint16_t)tid;
+    if (tid < s.head + (s.last - rest)) {
+      const int v = tid < s.head ? s.first + tid : rest + tid - s.head;
+      push(Elem<E>::get(x + v), v);
+    }
+  }
+  sync_group<G>();
+  const unsigned per = (unsigned)(s.pieces + G - 1) / G, items = per * (unsigned)sh.hots;
+  const uint4* p = reinterpret_cast<const uint4*>(x + body);
+  for (unsigned i = tid; i < items; i += G * kUnroll) {
+    uint4 v[kUnroll];
+    int at[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const unsigned item = i + u * G, h = item / per;
+      at[u] = item < items ? (int)(sh.hot[h] + (item - h * per) * G) : s.pieces;
+      v[u] = at[u] < s.pieces ? load16(p + at[u]) : no_piece(Elem<E>::kLowest);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      if (at[u] >= s.pieces) continue;
+      const uint4 one[1] = {v[u]};
+      if (!(Elem<E>::top(one) >= bound)) continue;
+      float f[8];
+      each<E>(v[u], f);
+#pragma unroll
+      for (int j = 0; j < N; ++j) push(f[j], body + at[u] * N + j);
+    }
+  }
+  sync_group<G>();
+  const int n = sh.keys;
+  if (n <= Top<G>::kKeys) rank_keys<G>(sh, n, k, tid);
+  else top_in_steps<E, G>(x, s, tid, k, sh);
+}
+
+// ---- a row -------------------------------------------------------------------------
+
+__device__ __forceinline__ int cluster_ranks() {
+  int n;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+  return n;
+}
+__device__ __forceinline__ int cluster_rank() {
+  int n;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(n));
+  return n;
+}
+
+template <int G>
+struct Shared {
+  Top<G> top;
+  float4 part[G / 32];
+};
+// What the CTAs of a cluster hand to its first one.
+struct Gathered {
+  float3 part[kMaxCluster];
+  Key key[kMaxCluster * kMostTop];
+};
+
+// s and w of a slice whose exponents leave the range of the fast path, relative to its m.
+template <typename E, int G>
+__device__ __noinline__ float3 part_extreme(const E* x, Slice s, int tid, float m, float c, float4* red) {
+  float sum = 0.f, log = 0.f;
+  for (unsigned v = s.first + tid; v < (unsigned)s.last; v += G) {
+    const float f = Elem<E>::get(x + v), z = f == -INFINITY ? f : (f - m) * c, e = exp2f(z);
+    sum += e;
+    log += times_log(e, z);
+  }
+  sum = warp_sum(sum);
+  log = warp_sum(log);
+  if (G > 32) {
+    __syncthreads();
+    if (tid % 32 == 0) red[tid / 32] = make_float4(0.f, 0.f, sum, log);
+    __syncthreads();
+    sum = log = 0.f;
+    for (int i = 0; i < G / 32; ++i) {
+      sum += red[i].z;
+      log += red[i].w;
+    }
+  }
+  return make_float3(m, sum, log);
+}
+
+template <typename E, int G>
+__device__ __forceinline__ float3 row_part(const E* x, const Slice& s, int tid, const Scores& a, Part& o, float4* red) {
+  o = slice_part<E, G>(x, s, tid, a.c);
+  Part q = warp_merge(o, a.c);
+  if (G > 32) {
+    const int lane = tid % 32;
+    if (lane == 0) red[tid / 32] = make_float4(q.m, q.M, q.s, q.w);
+    __syncthreads();
+    q = Part();
+    if (lane < G / 32) {
+      const float4 r = red[lane];
+      q.m = r.x; q.M = r.y; q.s = r.z; q.w = r.w;
+    }
+    q = warp_merge(q, a.c);
+  }
+  // so small a c that an element below -2^100 may count, or so large that x c overflowed
+  const bool slow = is_extreme(q.m, a.c) || a.c < 0x1p-70f || (isnan(q.w) && !isnan(q.s));
+  return slow ? part_extreme<E, G>(x, s, tid, q.m, a.c, red) : at_m(q, a.c);
+}
+
+// m, L and H of a row from the sums relative to m.
+__device__ __forceinline__ float3 finish(const float3& q) {
+  if (q.x == -INFINITY) return make_float3(q.x, NAN, NAN);
+  return make_float3(q.x, logf(q.y), logf(q.y) - kLn2 * (q.z / q.y));
+}
+// Row t's results, by lane `tid` of the threads that have them all.
+__device__ __forceinline__ void write_row(const Scores& a, int64_t t, float3 r, float xy, const Key* best, int tid) {
+  if (tid < a.k) {
+    const Key q = best[tid];
+    a.top[t * a.k + tid] = q ? class_of(q) : -1;
+    a.top_logp[t * a.k + tid] = q ? (value_of(q) - r.x) * a.inv_tau - r.y : -INFINITY;
+  }
+  if (tid) return;
+  if (a.logp) a.logp[t] = (xy - r.x) * a.inv_tau - r.y;
+  a.entropy[t] = r.z;
+  a.stats[t] = make_float2(r.x, r.y);
+}
+__device__ __forceinline__ void write_none(const Scores& a, int64_t t, int tid) {
+  if (tid < a.k) {
+    a.top[t * a.k + tid] = -1;
+    a.top_logp[t * a.k + tid] = -INFINITY;
+  }
+  if (tid) return;
+  if (a.logp) a.logp[t] = 0.f;
+  a.entropy[t] = 0.f;
+  a.stats[t] = make_float2(0.f, 0.f);
+}
+
+// A row per warp (G = 32), CTA or cluster of CTAs.
+template <typename E, int G>
+__global__ void __launch_bounds__(kThreads) scores_kernel(Scores a) {
+  extern __shared__ __align__(16) unsigned char raw[];
+  Shared<G>& sh = reinterpret_cast<Shared<G>*>(raw)[G == 32 ? threadIdx.x / 32 : 0];
+  const int rank = G == 32 ? 0 : cluster_rank(), ranks = G == 32 ? 1 : cluster_ranks();
+  const int tid = threadIdx.x % G;
+  const int64_t t = G == 32 ? blockIdx.x * (int64_t)kWarps + threadIdx.x / 32 : blockIdx.x / ranks;
+  if (t >= a.T) return;
+  const int32_t y = a.y ? a.y[t] : 0;
+  if (y < 0) {
+    if (rank == 0) write_none(a, t, tid);
+    return;
+  }
+  // a CTA's shared memory may be written by another one of its cluster only once it runs
+  if (ranks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   const E* x = static_cast<const E*>(a.x) + t * a.ld;
-  float m = -INFINITY, s = 0.f, w = 0.f;
-  for (unsigned v = tid; v < (unsigned)a.V; v += kThreads) m = fmaxf(m, Elem<E>::get(x + v));
-  m = block_max(m, red);
-  for (unsigned v = tid; v < (unsigned)a.V; v += kThreads) {
-    const float z = (Elem<E>::get(x + v) - m) * a.inv_tau, e = expf(z);
-    s += e;
-    w -= times_log(e, z);
+  const float xy = a.y && y < a.V ? Elem<E>::get(x + y) : NAN;
+  const Slice s = slice_of(x, a.V, rank, ranks);
+  Part mine;
+  float3 q = row_part<E, G>(x, s, tid, a, mine, sh.part);
+  if (a.k) slice_top<E, G>(x, s, tid, a.k, mine.m, sh.top);
+  if (ranks == 1) {
+    write_row(a, t, finish(q), xy, sh.top.best, tid);
+    return;
   }
-  s = block_add(s, red);
-  w = block_add(w, red);
-  const float L = logf(s);
+  Gathered& all = *reinterpret_cast<Gathered*>(raw + (sizeof(Shared<G>) + 15) / 16 * 16);
+  __syncwarp();
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  auto first = [](const void* p) {                           // the same place in the cluster's first CTA
+    uint32_t at;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"(smem_u32(p)));
+    return at;
+  };
   if (tid == 0) {
-    if (a.logp) a.logp[t] = y < a.V ? (Elem<E>::get(x + y) - m) * a.inv_tau - L : NAN;
-    a.entropy[t] = L + w / s;
-    a.stats[t] = make_float2(m, L);
+    const uint32_t at = first(&all.part[rank]);
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(q.x) : "memory");
+    asm volatile("st.shared::cluster.f32 [%0 + 4], %1;" ::"r"(at), "f"(q.y) : "memory");
+    asm volatile("st.shared::cluster.f32 [%0 + 8], %1;" ::"r"(at), "f"(q.z) : "memory");
   }
-  unsigned long long before = ~0ull;
-  for (int j = 0; j < a.k; ++j) {
-    if (tid == 0) best = 0;
+  if (tid < a.k)
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(first(&all.key[rank * a.k + tid])), "l"(sh.top.best[tid]) : "memory");
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (rank) return;
+  // parts relative to their own m: 2^((m_i - m) c) each
+  float m = -INFINITY, sum = 0.f, log = 0.f;
+  for (int i = 0; i < ranks; ++i) m = fmaxf(m, all.part[i].x);
+  for (int i = 0; i < ranks; ++i) {
+    const float3 p = all.part[i];
+    const float d = p.x == m ? 0.f : fmaxf((p.x - m) * a.c, -1e4f), f = ex2(d);
+    sum += p.y * f;
+    log += f * fmaf(d, p.y, p.z);
+  }
+  if (a.k) {
+    for (int i = tid; i < ranks * a.k; i += G) sh.top.key[i] = all.key[i];
     __syncthreads();
-    unsigned long long mine = 0;
-    for (unsigned v = tid; v < (unsigned)a.V; v += kThreads) {
-      const float f = Elem<E>::get(x + v) + 0.f;
-      const uint32_t b = __float_as_uint(f);
-      const unsigned long long key =
-          (unsigned long long)(b ^ ((int32_t)b < 0 ? 0xffffffffu : 0x80000000u)) << 32 | (0xffffffffu - v);
-      if (f > -INFINITY && key < before && key > mine) mine = key;
+    rank_keys<G>(sh.top, ranks * a.k, a.k, tid);
+  }
+  write_row(a, t, finish(make_float3(m, sum, log)), xy, sh.top.best, tid);
+}
+
+// ---- gradient ----------------------------------------------------------------------
+
+// -p (a + b (q + H)) / tau is 2^z (at0 + at_z z) with z = x c - M, as q is linear in z.
+struct Slope {
+  float m, M, c, at0, at_z, at_y;
+  int y;
+  bool extreme;
+  float L, H, a, b, inv_tau;          // extreme rows
+};
+__device__ __forceinline__ Slope slope_of(float2 st, float H, float a, float b, float inv_tau, float c, int y) {
+  Slope r;
+  r.m = st.x; r.c = c; r.y = y;
+  r.M = ref_of(st.x, c);
+  r.extreme = is_extreme(st.x, c);
+  r.L = st.y; r.H = H; r.a = a; r.b = b; r.inv_tau = inv_tau;
+  const float l2 = fmaf(st.x, c, -r.M) + st.y * kLog2e;       // log2 of the sum at M
+  const float scale = -inv_tau * exp2f(-l2);
+  r.at0 = scale * fmaf(b, fmaf(-kLn2, l2, H), a);
+  r.at_z = scale * b * kLn2;
+  r.at_y = a * inv_tau;
+  return r;
+}
+__device__ __forceinline__ float slope_at(float x, bool target, const Slope& r) {
+  if (r.extreme) {
+    const float q = (x - r.m) * r.inv_tau - r.L;
+    return (-expf(q) * fmaf(r.b, fmaxf(q + r.H, -1e4f), r.a) + (target ? r.a : 0.f)) * r.inv_tau;
+  }
+  const float z = fmaxf(fmaf(x, r.c, -r.M), -1e4f);
+  return fmaf(ex2(z), fmaf(z, r.at_z, r.at0), target ? r.at_y : 0.f);
+}
+template <typename E>
+__device__ __forceinline__ void slope_piece(const uint4& v, E* out, bool wide, const Slope& r) {
+  constexpr int N = Elem<E>::N;
+  Pair f[N / 2];
+  Elem<E>::widen(v, f);
+  const Pair c2 = pair(r.c, r.c), M2 = pair(-r.M, -r.M), k0 = pair(r.at0, r.at0), kz = pair(r.at_z, r.at_z);
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    float lo, hi;
+    split(fma2(f[i], c2, M2), lo, hi);
+    const Pair z = pair(fmaxf(lo, -1e4f), fmaxf(hi, -1e4f));
+    f[i] = mul2(ex2_2(z), fma2(z, kz, k0));
+  }
+  if (wide) {
+    store16(reinterpret_cast<uint4*>(out), Elem<E>::narrow(f));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      float lo, hi;
+      split(f[i], lo, hi);
+      Elem<E>::put(out + 2 * i, lo);
+      Elem<E>::put(out + 2 * i + 1, hi);
     }
-    atomicMax(&best, mine);
-    __syncthreads();
-    before = best;
-    if (tid == 0) {
-      const int32_t at = before ? (int32_t)(0xffffffffu - (uint32_t)before) : -1;
-      top[j] = at;
-      top_logp[j] = before ? (Elem<E>::get(x + at) - m) * a.inv_tau - L : -INFINITY;
-    }
-    __syncthreads();
   }
 }
 
-template <typename E>
-__global__ void __launch_bounds__(kThreads) scores_grad_kernel(Scores a, const float* dlogp, const float* dentropy) {
-  const int64_t t = blockIdx.x;
+// A row, or one of its `parts`, per group: nothing is exchanged between them.  In place too: a thread
+// reads what it writes before it does, and the target's logit, which the thread of its piece writes again.
+template <typename E, int G>
+__global__ void __launch_bounds__(kThreads) scores_grad_kernel(Scores a, int parts, const float* dlogp, const float* dentropy) {
+  constexpr int N = Elem<E>::N;
+  const int rank = G == 32 ? 0 : blockIdx.x % parts, ranks = G == 32 ? 1 : parts;
+  const int tid = threadIdx.x % G;
+  const int64_t t = G == 32 ? blockIdx.x * (int64_t)kWarps + threadIdx.x / 32 : blockIdx.x / parts;
+  if (t >= a.T) return;
   const int32_t y = a.y ? a.y[t] : 0;
   const E* x = static_cast<const E*>(a.x) + t * a.ld;
   E* g = static_cast<E*>(a.g) + t * a.ldg;
+  const Slice s = slice_of(x, a.V, rank, ranks);
   const float da = dlogp && y >= 0 ? dlogp[t] : 0.f, db = dentropy && y >= 0 ? dentropy[t] : 0.f;
   const float2 st = a.stats[t];
   const float H = db != 0.f ? a.entropy[t] : 0.f;
-  float fill = 0.f;
-  if (da != 0.f || db != 0.f) fill = isnan(da) || isnan(db) || isnan(st.y) || isnan(H) || (da != 0.f && y >= a.V) ? NAN : 1.f;
-  for (unsigned v = threadIdx.x; v < (unsigned)a.V; v += kThreads) {
-    float d = fill;
-    if (fill == 1.f) {
-      const float q = (Elem<E>::get(x + v) - st.x) * a.inv_tau - st.y;
-      d = -expf(q) * (da + db * fmaxf(q + H, -1e4f));
-      d = (d + (da != 0.f && (int)v == y ? da : 0.f)) * a.inv_tau;
-    }
-    Elem<E>::put(g + v, d);
+  const bool none = da == 0.f && db == 0.f;
+  if (none || isnan(da) || isnan(db) || isnan(st.y) || isnan(H) || (da != 0.f && y >= a.V)) {
+    slice_fill<E, G>(g, s.first, s.last, tid, none ? 0.f : NAN);
+    return;
   }
+  const int target = da != 0.f ? y : -1;
+  const float xy = target >= 0 ? Elem<E>::get(x + target) : 0.f;
+  const Slope r = slope_of(st, H, da, db, a.inv_tau, a.c, target);
+  if (r.extreme) {
+    for (unsigned v = s.first + tid; v < (unsigned)s.last; v += G)
+      Elem<E>::put(g + v, slope_at(Elem<E>::get(x + v), (int)v == target, r));
+    return;
+  }
+  const int body = s.first + s.head, rest = body + s.pieces * N;
+  if (tid < s.head + (s.last - rest)) {
+    const int v = tid < s.head ? s.first + tid : rest + tid - s.head;
+    Elem<E>::put(g + v, slope_at(Elem<E>::get(x + v), v == target, r));
+  }
+  const uint4* p = reinterpret_cast<const uint4*>(x + body);
+  const bool wide = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(g)) & 15) == 0;
+  for (int i = tid; i < s.pieces; i += G * kUnroll) {
+    uint4 v[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+      if (i + u * G < s.pieces) v[u] = load16(p + i + u * G);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+      if (i + u * G < s.pieces) slope_piece<E>(v[u], g + body + (i + u * G) * N, wide, r);
+  }
+  const int at = target - body;
+  if (target >= 0 && at >= 0 && at < s.pieces * N && at / N % G == tid) Elem<E>::put(g + target, slope_at(xy, true, r));
 }
 
 // ---- host --------------------------------------------------------------------
@@ -160,7 +607,67 @@ Scores scores_of(const pgc_logits* z) {
   a.x = z->x; a.g = z->grad; a.y = z->target; a.T = z->rows; a.ld = z->ld; a.ldg = z->grad_ld;
   a.V = (int32_t)z->classes;
   a.inv_tau = 1.f / z->temperature;
+  a.c = a.inv_tau * kLog2e;
   return a;
+}
+
+int sm_count() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return 148;
+  return n;
+}
+
+// Rows as in the losses' streaming passes: a warp takes one up to 4 KB, or 24 KB
+// where there are rows for all warps; few long rows are split over a cluster while the SMs hold more CTAs and a part
+// stays above 4 KB.
+constexpr int64_t kWarpRowBytes = 4 * 1024, kWarpManyRowsBytes = 24 * 1024;
+struct Shape {
+  bool warp;
+  int ranks;
+  unsigned grid;
+};
+Shape shape_of(const pgc_logits* z, int k) {
+  const int64_t bytes = z->classes * (z->dtype == PGC_BF16 ? 2 : 4), sms = sm_count();
+  Shape s{k <= kWarpTop && (bytes <= kWarpRowBytes || (bytes <= kWarpManyRowsBytes && z->rows >= 32 * sms)), 1, 0};
+  if (s.warp) {
+    s.grid = (unsigned)((z->rows + kWarps - 1) / kWarps);
+    return s;
+  }
+  while (s.ranks < kMaxCluster && z->rows * s.ranks * 2 <= 2 * sms && bytes / (s.ranks * 2) >= kWarpRowBytes) s.ranks *= 2;
+  s.grid = (unsigned)(z->rows * s.ranks);
+  return s;
+}
+
+template <typename E>
+cudaError_t launch_scores(const Scores& a, const Shape& s, cudaStream_t st) {
+  const auto kernel = s.warp ? scores_kernel<E, 32> : scores_kernel<E, kThreads>;
+  size_t smem = s.warp ? sizeof(Shared<32>) * kWarps : sizeof(Shared<kThreads>);
+  if (s.ranks > 1) smem = (smem + 15) / 16 * 16 + sizeof(Gathered);
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)s.ranks;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(s.grid);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = &attr;
+  cfg.numAttrs = s.ranks > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+// The gradient takes a longer row in parts of 32 KB at least, few rows in as many as a cluster would have CTAs.
+constexpr int64_t kGradPartBytes = 32 * 1024;
+template <typename E>
+cudaError_t launch_grad(const Scores& a, const Shape& s, const float* dlogp, const float* dentropy, cudaStream_t st) {
+  const int64_t bytes = a.V * (int64_t)sizeof(E), most = INT32_MAX / a.T;
+  const int parts = s.warp ? 1 : (int)std::min(std::max<int64_t>(s.ranks, bytes / kGradPartBytes), most);
+  const unsigned grid = s.warp ? s.grid : (unsigned)(a.T * parts);
+  if (s.warp) scores_grad_kernel<E, 32><<<grid, kThreads, 0, st>>>(a, parts, dlogp, dentropy);
+  else scores_grad_kernel<E, kThreads><<<grid, kThreads, 0, st>>>(a, parts, dlogp, dentropy);
+  return cudaGetLastError();
 }
 
 }  // namespace
@@ -184,9 +691,8 @@ int pgc_token_scores(const pgc_logits *z, int32_t k, float *logp, float *entropy
   a.k = k; a.logp = logp; a.entropy = entropy; a.top = top; a.top_logp = top_logp;
   a.stats = reinterpret_cast<float2*>(stats);
   const cudaStream_t st = (cudaStream_t)stream;
-  if (z->dtype == PGC_BF16) scores_kernel<__nv_bfloat16><<<(unsigned)z->rows, kThreads, 0, st>>>(a);
-  else scores_kernel<float><<<(unsigned)z->rows, kThreads, 0, st>>>(a);
-  return report_cuda(cudaGetLastError());
+  const Shape s = shape_of(z, k);
+  return report_cuda(z->dtype == PGC_BF16 ? launch_scores<__nv_bfloat16>(a, s, st) : launch_scores<float>(a, s, st));
 }
 
 int pgc_token_scores_grad(const pgc_logits *z, const float *stats, const float *entropy, const float *dlogp,
@@ -200,9 +706,9 @@ int pgc_token_scores_grad(const pgc_logits *z, const float *stats, const float *
   a.stats = reinterpret_cast<float2*>(const_cast<float*>(stats));
   a.entropy = const_cast<float*>(entropy);
   const cudaStream_t st = (cudaStream_t)stream;
-  if (z->dtype == PGC_BF16) scores_grad_kernel<__nv_bfloat16><<<(unsigned)z->rows, kThreads, 0, st>>>(a, dlogp, dentropy);
-  else scores_grad_kernel<float><<<(unsigned)z->rows, kThreads, 0, st>>>(a, dlogp, dentropy);
-  return report_cuda(cudaGetLastError());
+  const Shape s = shape_of(z, 0);
+  return report_cuda(z->dtype == PGC_BF16 ? launch_grad<__nv_bfloat16>(a, s, dlogp, dentropy, st)
+                                          : launch_grad<float>(a, s, dlogp, dentropy, st));
 }
 
 }  // extern "C"
