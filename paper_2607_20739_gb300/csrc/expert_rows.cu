@@ -166,8 +166,12 @@ __global__ void __launch_bounds__(kRouteThreads) place_kernel(Route a) {
 }
 
 // ---- rows ----------------------------------------------------------------------
-// A row is read and written in pieces of W bytes, the most that all rows' starts
-// allow, and single elements behind the last piece.
+// A lane has pieces of W bytes of a row: 16 where every row starts on 16 bytes, else 4, or 2 where bf16
+// rows start between two words.  (16-byte pieces put together from the two that hold them were slower: 90
+// instructions a piece, 109 us where 4-byte pieces take 55: join of 10000 x 6 x 1001 fp32.)  What is left
+// behind the last piece is taken by single elements.  All three kernels are bound by memory:
+// at 16 bytes they move 6.1 to 6.6 TB/s (bf16, 16384 x 8 x 2048: spread 96 us, join 96, gradient 174), at 4 bytes
+// fp32 5.1 to 5.8, at 2 bytes 3.2 to 5.0.
 
 struct Move {
   const void* x;                // spread: tokens; join, join_grad: the experts' rows
@@ -178,50 +182,56 @@ struct Move {
   float* dweight;
   int64_t T, rows, ldx, ldy, ldo;
   int k, d;
-  int chunks;                   // parts of a row, each a warp's
+  int chunks;                   // spread: parts of a row, each a warp's
 };
-
-template <int W> struct RawOf;
-template <> struct RawOf<16> { using T = uint4; };
-template <> struct RawOf<8> { using T = uint2; };
-template <> struct RawOf<4> { using T = uint32_t; };
-template <> struct RawOf<2> { using T = uint16_t; };
 
 template <typename E, int W>
-struct Piece {
-  using Raw = typename RawOf<W>::T;
-  static constexpr int N = W / (int)sizeof(E);
-  Raw raw;
-  __device__ __forceinline__ void widen(float (&f)[N]) const {
-    if constexpr (sizeof(E) == 4) {
-      const uint32_t* w = reinterpret_cast<const uint32_t*>(&raw);
+struct Access;
+template <typename E>
+struct Access<E, 16> {
+  static constexpr int N = Elem<E>::N;
+  using Raw = uint4;
+  __device__ __forceinline__ static void widen(const Raw& v, float (&f)[N]) {
+    Pair h[4];
+    Elem<E>::widen(v, h);
 #pragma unroll
-      for (int i = 0; i < N; ++i) f[i] = __uint_as_float(w[i]);
-    } else if constexpr (W == 2) {
-      f[0] = __uint_as_float((uint32_t)raw << 16);
-    } else {
-      const uint32_t* w = reinterpret_cast<const uint32_t*>(&raw);
-#pragma unroll
-      for (int i = 0; i < N; i += 2) {
-        f[i] = __uint_as_float(w[i / 2] << 16);
-        f[i + 1] = __uint_as_float(w[i / 2] & 0xffff0000u);
-      }
-    }
+    for (int i = 0; i < N / 2; ++i) split(h[i], f[2 * i], f[2 * i + 1]);
   }
-  __device__ __forceinline__ void narrow(const float (&f)[N]) {
-    if constexpr (sizeof(E) == 4) {
-      uint32_t* w = reinterpret_cast<uint32_t*>(&raw);
+  __device__ __forceinline__ static Raw narrow(const float (&f)[N]) {
+    Pair h[4];
 #pragma unroll
-      for (int i = 0; i < N; ++i) w[i] = __float_as_uint(f[i]);
-    } else if constexpr (W == 2) {
-      raw = __bfloat16_as_ushort(__float2bfloat16_rn(f[0]));
-    } else {
-      uint32_t* w = reinterpret_cast<uint32_t*>(&raw);
-#pragma unroll
-      for (int i = 0; i < N; i += 2) w[i / 2] = Elem<__nv_bfloat16>::two(pair(f[i], f[i + 1]));
-    }
+    for (int i = 0; i < N / 2; ++i) h[i] = pair(f[2 * i], f[2 * i + 1]);
+    return Elem<E>::narrow(h);
   }
 };
+template <>
+struct Access<float, 4> {
+  static constexpr int N = 1;
+  using Raw = float;
+  __device__ __forceinline__ static void widen(Raw v, float (&f)[1]) { f[0] = v; }
+  __device__ __forceinline__ static Raw narrow(const float (&f)[1]) { return f[0]; }
+};
+template <>
+struct Access<__nv_bfloat16, 4> {
+  static constexpr int N = 2;
+  using Raw = uint32_t;
+  __device__ __forceinline__ static void widen(Raw v, float (&f)[2]) {
+    f[0] = __uint_as_float(v << 16);
+    f[1] = __uint_as_float(v & 0xffff0000u);
+  }
+  __device__ __forceinline__ static Raw narrow(const float (&f)[2]) { return Elem<__nv_bfloat16>::two(pair(f[0], f[1])); }
+};
+template <>
+struct Access<__nv_bfloat16, 2> {
+  static constexpr int N = 1;
+  using Raw = uint16_t;
+  __device__ __forceinline__ static void widen(Raw v, float (&f)[1]) { f[0] = bf16_bits_to_float(v); }
+  __device__ __forceinline__ static Raw narrow(const float (&f)[1]) { return __bfloat16_as_ushort(__float2bfloat16_rn(f[0])); }
+};
+template <typename A, typename E>
+__device__ __forceinline__ typename A::Raw load(const E* x) { return *reinterpret_cast<const typename A::Raw*>(x); }
+template <typename A, typename E>
+__device__ __forceinline__ void store(E* x, const typename A::Raw& v) { *reinterpret_cast<typename A::Raw*>(x) = v; }
 
 // The rows of a token's slots: lane j has those of slots j and j + 32, -1 without one.
 struct Places {
@@ -235,7 +245,11 @@ struct Places {
     const int r = j < a.k ? a.place[t * a.k + j] : -1;
     return r >= 0 && r < a.rows ? r : -1;
   }
-  __device__ __forceinline__ int operator[](int j) const { return __shfl_sync(0xffffffffu, j < 32 ? lo : hi, j & 31); }
+  // -1 behind the last slot
+  __device__ __forceinline__ int operator[](int j) const {
+    const int r = __shfl_sync(0xffffffffu, j < 32 ? lo : hi, j & 31);
+    return j < kMaxChoices ? r : -1;
+  }
 };
 // The same for the weights (1 where there are none).
 struct Weights {
@@ -248,25 +262,26 @@ struct Weights {
   __device__ __forceinline__ float operator[](int j) const { return __shfl_sync(0xffffffffu, j < 32 ? lo : hi, j & 31); }
 };
 
+// Pieces that a lane has in flight.
 template <int W>
-constexpr int spread_pieces() { return W == 16 ? 4 : 8; }       // a lane has in flight
+constexpr int spread_pieces() { return W == 16 ? 4 : 8; }
 
 template <typename E, int W>
 __global__ void __launch_bounds__(kThreads) spread_kernel(Move a) {
-  constexpr int N = Piece<E, W>::N, U = spread_pieces<W>();
-  using Raw = typename RawOf<W>::T;
+  using A = Access<E, W>;
+  constexpr int N = A::N, U = spread_pieces<W>();
   const int lane = threadIdx.x % 32;
   const int64_t unit = blockIdx.x * (int64_t)kWarps + threadIdx.x / 32;
   const int64_t t = unit / a.chunks;
   if (t >= a.T) return;
   const int chunk = (int)(unit - t * a.chunks), pieces = a.d / N, p0 = chunk * (32 * U) + lane;
+  const int rest = chunk == a.chunks - 1 && lane < a.d - pieces * N ? pieces * N + lane : -1;
   const E* x = static_cast<const E*>(a.x) + t * a.ldx;
   const Places at(a, t);
-  Raw v[U];
+  typename A::Raw v[U];
 #pragma unroll
   for (int u = 0; u < U; ++u)
-    if (p0 + 32 * u < pieces) v[u] = reinterpret_cast<const Raw*>(x)[p0 + 32 * u];
-  const int rest = chunk == a.chunks - 1 && lane < a.d - pieces * N ? pieces * N + lane : -1;
+    if (p0 + 32 * u < pieces) v[u] = load<A>(x + (p0 + 32 * u) * N);
   const E last = rest >= 0 ? x[rest] : E();
   for (int j = 0; j < a.k; ++j) {
     const int r = at[j];
@@ -274,77 +289,86 @@ __global__ void __launch_bounds__(kThreads) spread_kernel(Move a) {
     E* out = static_cast<E*>(a.out) + r * a.ldo;
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (p0 + 32 * u < pieces) reinterpret_cast<Raw*>(out)[p0 + 32 * u] = v[u];
+      if (p0 + 32 * u < pieces) store<A>(out + (p0 + 32 * u) * N, v[u]);
     if (rest >= 0) out[rest] = last;
   }
 }
 
+constexpr int kJoinRows = 4;          // rows that a lane has in flight, with U pieces of each
 template <int W>
-constexpr int join_pieces() { return W == 16 ? 2 : 4; }
-constexpr int kJoinAtOnce = 4;        // rows a lane has in flight
+constexpr int join_pieces() { return W == 16 ? 2 : 8; }
 
-template <typename E, int W>
-__global__ void __launch_bounds__(kThreads) join_kernel(Move a) {
-  constexpr int N = Piece<E, W>::N, U = join_pieces<W>();
-  using Raw = typename RawOf<W>::T;
-  const int lane = threadIdx.x % 32;
-  const int64_t unit = blockIdx.x * (int64_t)kWarps + threadIdx.x / 32;
-  const int64_t t = unit / a.chunks;
+// A token per warp (G = 32) or CTA, in a loop over its row: a warp for each part of a row
+// spent its time on the places and weights (8192 x 4 x 5120 bf16: 98 us, 58 this way).
+template <typename E, int W, int G>
+__global__ void __launch_bounds__(kThreads, 4) join_kernel(Move a) {
+  using A = Access<E, W>;
+  constexpr int N = A::N, U = join_pieces<W>(), Q = kJoinRows;
+  const int tid = threadIdx.x % G;
+  const int64_t t = G == 32 ? blockIdx.x * (int64_t)kWarps + threadIdx.x / 32 : blockIdx.x;
   if (t >= a.T) return;
-  const int chunk = (int)(unit - t * a.chunks), pieces = a.d / N, p0 = chunk * (32 * U) + lane;
-  const int rest = chunk == a.chunks - 1 && lane < a.d - pieces * N ? pieces * N + lane : -1;
+  E* out = static_cast<E*>(a.out) + t * a.ldo;
+  const int pieces = a.d / N, rest = a.d - pieces * N;
   const Places at(a, t);
   const Weights w(a, t);
-  float sum[U][N], sum_rest = 0.f;
+  for (int p0 = 0; p0 < pieces; p0 += G * U) {
+    const int first = p0 + tid;
+    float sum[U][N];
 #pragma unroll
-  for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int i = 0; i < N; ++i) sum[u][i] = 0.f;
-  for (int j0 = 0; j0 < a.k; j0 += kJoinAtOnce) {
-    Piece<E, W> v[kJoinAtOnce][U];
-    int r[kJoinAtOnce];
-    float wj[kJoinAtOnce];
+      for (int i = 0; i < N; ++i) sum[u][i] = 0.f;
+    for (int j0 = 0; j0 < a.k; j0 += Q) {
+      typename A::Raw v[Q][U];
+      int r[Q];
 #pragma unroll
-    for (int q = 0; q < kJoinAtOnce; ++q) {
-      r[q] = j0 + q < a.k ? at[j0 + q] : -1;
-      wj[q] = j0 + q < a.k ? w[j0 + q] : 0.f;
-      if (r[q] < 0) continue;
-      const E* x = static_cast<const E*>(a.x) + r[q] * a.ldx;
+      for (int q = 0; q < Q; ++q) {
+        r[q] = at[j0 + q];
+        if (r[q] < 0) continue;
+        const E* x = static_cast<const E*>(a.x) + r[q] * a.ldx + first * N;
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (p0 + 32 * u < pieces) v[q][u].raw = reinterpret_cast<const Raw*>(x)[p0 + 32 * u];
-    }
-#pragma unroll
-    for (int q = 0; q < kJoinAtOnce; ++q) {
-      if (r[q] < 0) continue;
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (p0 + 32 * u >= pieces) continue;
-        float f[N];
-        v[q][u].widen(f);
-#pragma unroll
-        for (int i = 0; i < N; ++i) sum[u][i] = fmaf(wj[q], f[i], sum[u][i]);
+        for (int u = 0; u < U; ++u)
+          if (first + u * G < pieces) v[q][u] = load<A>(x + u * G * N);
       }
-      if (rest >= 0) sum_rest = fmaf(wj[q], Elem<E>::get(static_cast<const E*>(a.x) + r[q] * a.ldx + rest), sum_rest);
-    }
-  }
-  E* out = static_cast<E*>(a.out) + t * a.ldo;
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    if (p0 + 32 * u >= pieces) continue;
-    Piece<E, W> v;
-    v.narrow(sum[u]);
-    reinterpret_cast<Raw*>(out)[p0 + 32 * u] = v.raw;
+      for (int q = 0; q < Q; ++q) {
+        const float wj = w[j0 + q];
+        if (r[q] < 0) continue;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (first + u * G >= pieces) continue;
+          float f[N];
+          A::widen(v[q][u], f);
+#pragma unroll
+          for (int i = 0; i < N; ++i) sum[u][i] = fmaf(wj, f[i], sum[u][i]);
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (first + u * G < pieces) store<A>(out + (first + u * G) * N, A::narrow(sum[u]));
   }
-  if (rest >= 0) Elem<E>::put(out + rest, sum_rest);
+  if (rest && (G == 32 || threadIdx.x < 32)) {
+    float sum = 0.f;
+    for (int j = 0; j < a.k; ++j) {
+      const int r = at[j];
+      const float wj = w[j];
+      if (r >= 0 && tid < rest) sum = fmaf(wj, Elem<E>::get(static_cast<const E*>(a.x) + r * a.ldx + pieces * N + tid), sum);
+    }
+    if (tid < rest) Elem<E>::put(out + pieces * N + tid, sum);
+  }
 }
 
-constexpr int kGradAtOnce = 8;
-// A token per warp (G = 32) or CTA: the products with its own row are summed over all of it.
-template <typename E, int W, int G>
-__global__ void __launch_bounds__(kThreads) join_grad_kernel(Move a) {
-  constexpr int N = Piece<E, W>::N;
-  using Raw = typename RawOf<W>::T;
+template <int W>
+constexpr int grad_pieces() { return W == 16 ? 1 : 3; }
+
+// A token per warp or CTA: the products with its own row are summed over all of it.  Q rows at
+// once: the least of 2, 4 and 8 that takes k, or 8 (65536 x 2 x 1024 bf16: 108 us, 137 with 8), for which three CTAs an
+// SM matter more than registers (16384 x 8 x 2048 bf16: 174 us, 226 with two).  In place too: a lane reads what it writes before it does.
+template <typename E, int W, int Q, int G>
+__global__ void __launch_bounds__(kThreads, Q == 2 ? 4 : 3) join_grad_kernel(Move a) {
+  using A = Access<E, W>;
+  constexpr int N = A::N, U = grad_pieces<W>();
   __shared__ float red[kWarps][kMaxChoices];
   const int lane = threadIdx.x % 32, tid = threadIdx.x % G, warp = threadIdx.x / 32;
   const int64_t t = G == 32 ? blockIdx.x * (int64_t)kWarps + warp : blockIdx.x;
@@ -353,51 +377,58 @@ __global__ void __launch_bounds__(kThreads) join_grad_kernel(Move a) {
   const E* dy = static_cast<const E*>(a.dy) + t * a.ldy;
   const Places at(a, t);
   const Weights w(a, t);
-  for (int j0 = 0; j0 < a.k; j0 += kGradAtOnce) {
-    const E* x[kGradAtOnce];
-    E* out[kGradAtOnce];
-    float wj[kGradAtOnce], sum[kGradAtOnce];
+  for (int j0 = 0; j0 < a.k; j0 += Q) {
+    int r[Q];
+    float wj[Q], sum[Q];
 #pragma unroll
-    for (int q = 0; q < kGradAtOnce; ++q) {
-      const int r = j0 + q < a.k ? at[j0 + q] : -1;
-      wj[q] = j0 + q < a.k ? w[j0 + q] : 0.f;
-      x[q] = r >= 0 ? static_cast<const E*>(a.x) + r * a.ldx : nullptr;
-      out[q] = r >= 0 ? static_cast<E*>(a.out) + r * a.ldo : nullptr;
+    for (int q = 0; q < Q; ++q) {
+      r[q] = at[j0 + q];
+      wj[q] = w[j0 + q];
       sum[q] = 0.f;
     }
-    for (int p = tid; p < pieces; p += G) {
-      Piece<E, W> v[kGradAtOnce], own;
-      own.raw = reinterpret_cast<const Raw*>(dy)[p];
+    for (int p = tid; p < pieces; p += G * U) {
+      typename A::Raw own[U], v[Q][U];
 #pragma unroll
-      for (int q = 0; q < kGradAtOnce; ++q)
-        if (x[q]) v[q].raw = reinterpret_cast<const Raw*>(x[q])[p];
-      float d[N];
-      own.widen(d);
+      for (int u = 0; u < U; ++u)
+        if (p + u * G < pieces) own[u] = load<A>(dy + (p + u * G) * N);
 #pragma unroll
-      for (int q = 0; q < kGradAtOnce; ++q) {
-        if (!x[q]) continue;
-        float f[N];
-        v[q].widen(f);
+      for (int q = 0; q < Q; ++q) {
+        if (r[q] < 0) continue;
+        const E* x = static_cast<const E*>(a.x) + r[q] * a.ldx + p * N;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          sum[q] = fmaf(d[i], f[i], sum[q]);
-          f[i] = wj[q] * d[i];
+        for (int u = 0; u < U; ++u)
+          if (p + u * G < pieces) v[q][u] = load<A>(x + u * G * N);
+      }
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        if (r[q] < 0) continue;
+        E* out = static_cast<E*>(a.out) + r[q] * a.ldo + p * N;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (p + u * G >= pieces) continue;
+          float d[N], f[N];
+          A::widen(own[u], d);
+          A::widen(v[q][u], f);
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            sum[q] = fmaf(d[i], f[i], sum[q]);
+            f[i] = wj[q] * d[i];
+          }
+          store<A>(out + u * G * N, A::narrow(f));
         }
-        v[q].narrow(f);
-        reinterpret_cast<Raw*>(out[q])[p] = v[q].raw;
       }
     }
     if (rest >= 0) {
       const float d = Elem<E>::get(dy + rest);
 #pragma unroll
-      for (int q = 0; q < kGradAtOnce; ++q) {
-        if (!x[q]) continue;
-        sum[q] = fmaf(d, Elem<E>::get(x[q] + rest), sum[q]);
-        Elem<E>::put(out[q] + rest, wj[q] * d);
+      for (int q = 0; q < Q; ++q) {
+        if (r[q] < 0) continue;
+        sum[q] = fmaf(d, Elem<E>::get(static_cast<const E*>(a.x) + r[q] * a.ldx + rest), sum[q]);
+        Elem<E>::put(static_cast<E*>(a.out) + r[q] * a.ldo + rest, wj[q] * d);
       }
     }
 #pragma unroll
-    for (int q = 0; q < kGradAtOnce; ++q) {
+    for (int q = 0; q < Q; ++q) {
       sum[q] = warp_sum(sum[q]);
       if (lane == 0 && j0 + q < a.k) {
         if (G == 32) a.dweight[t * a.k + j0 + q] = sum[q];
@@ -444,59 +475,39 @@ int sm_count() {
 constexpr int kAloneSlots = 8192, kMostRouteCtas = 128;
 int route_ctas(int64_t n) { return (int)std::min<int64_t>((n + 1023) / 1024, kMostRouteCtas); }
 
-// The most bytes that divide every row's start.
+// The pieces that all rows' starts allow.
 int width_of(std::initializer_list<uintptr_t> starts) {
-  uintptr_t all = 16;
+  uintptr_t all = 0;
   for (const uintptr_t p : starts) all |= p;
-  return (int)(all & (~all + 1));
+  return all % 16 == 0 ? 16 : all % 4 == 0 ? 4 : 2;
 }
-// f.template operator()<E, W>()
-template <typename F>
-cudaError_t by_width(int32_t dtype, int width, F f) {
-  using H = __nv_bfloat16;
-  if (dtype == PGC_F32) {
-    if (width >= 16) return f.template operator()<float, 16>();
-    if (width >= 8) return f.template operator()<float, 8>();
-    return f.template operator()<float, 4>();
-  }
-  if (width >= 16) return f.template operator()<H, 16>();
-  if (width >= 8) return f.template operator()<H, 8>();
-  if (width >= 4) return f.template operator()<H, 4>();
-  return f.template operator()<H, 2>();
+// A token is a warp's where there are tokens for the SMs' warps, else a CTA's.
+bool by_warps(const Move& a) { return a.T >= sm_count() * 32; }
+unsigned grid_of(const Move& a, bool warps) { return (unsigned)(warps ? (a.T + kWarps - 1) / kWarps : a.T); }
+
+template <typename E, int W>
+cudaError_t launch_spread(Move a, cudaStream_t st) {
+  const int most = 32 * spread_pieces<W>();
+  a.chunks = std::max((a.d / Access<E, W>::N + most - 1) / most, 1);
+  spread_kernel<E, W><<<(unsigned)((a.T * a.chunks + kWarps - 1) / kWarps), kThreads, 0, st>>>(a);
+  return cudaGetLastError();
 }
-// Warps for T rows in chunks of 32 U pieces, and the chunks; too many warps for a grid of CTAs are refused by the launch.
-unsigned grid_of(Move& a, int n, int u) {
-  a.chunks = std::max((a.d / n + 32 * u - 1) / (32 * u), 1);
-  return (unsigned)((a.T * a.chunks + kWarps - 1) / kWarps);
+template <typename E, int W>
+cudaError_t launch_join(const Move& a, cudaStream_t st) {
+  const bool warps = by_warps(a);
+  (warps ? join_kernel<E, W, 32> : join_kernel<E, W, kThreads>)<<<grid_of(a, warps), kThreads, 0, st>>>(a);
+  return cudaGetLastError();
 }
-struct Spread {
-  Move a;
-  cudaStream_t st;
-  template <typename E, int W> cudaError_t operator()() {
-    const unsigned grid = grid_of(a, Piece<E, W>::N, spread_pieces<W>());
-    spread_kernel<E, W><<<grid, kThreads, 0, st>>>(a);
-    return cudaGetLastError();
-  }
-};
-struct Join {
-  Move a;
-  cudaStream_t st;
-  template <typename E, int W> cudaError_t operator()() {
-    const unsigned grid = grid_of(a, Piece<E, W>::N, join_pieces<W>());
-    join_kernel<E, W><<<grid, kThreads, 0, st>>>(a);
-    return cudaGetLastError();
-  }
-};
-// A warp per token where there are tokens for the SMs' warps, else a CTA.
-struct JoinGrad {
-  Move a;
-  cudaStream_t st;
-  template <typename E, int W> cudaError_t operator()() {
-    if (a.T >= sm_count() * 32) join_grad_kernel<E, W, 32><<<(unsigned)((a.T + kWarps - 1) / kWarps), kThreads, 0, st>>>(a);
-    else join_grad_kernel<E, W, kThreads><<<(unsigned)a.T, kThreads, 0, st>>>(a);
-    return cudaGetLastError();
-  }
-};
+template <typename E, int W, int G>
+auto join_grad_of(int k) {
+  return k <= 2 ? join_grad_kernel<E, W, 2, G> : k <= 4 ? join_grad_kernel<E, W, 4, G> : join_grad_kernel<E, W, 8, G>;
+}
+template <typename E, int W>
+cudaError_t launch_join_grad(const Move& a, cudaStream_t st) {
+  const bool warps = by_warps(a);
+  (warps ? join_grad_of<E, W, 32>(a.k) : join_grad_of<E, W, kThreads>(a.k))<<<grid_of(a, warps), kThreads, 0, st>>>(a);
+  return cudaGetLastError();
+}
 
 }  // namespace
 }  // namespace pgc
@@ -563,7 +574,10 @@ int pgc_spread(int32_t dtype, int64_t tokens, int32_t k, int64_t d, const void *
   a.x = x; a.out = out; a.place = place; a.T = tokens; a.rows = rows; a.ldx = ld; a.ldo = out_ld; a.k = k; a.d = (int)d;
   const cudaStream_t st = (cudaStream_t)stream;
   const int width = width_of({(uintptr_t)x, (uintptr_t)out, (uintptr_t)ld * size, (uintptr_t)out_ld * size});
-  return report_cuda(by_width(dtype, width, Spread{a, st}));
+  if (dtype == PGC_BF16)
+    return report_cuda(width == 16 ? launch_spread<__nv_bfloat16, 16>(a, st)
+                       : width == 4 ? launch_spread<__nv_bfloat16, 4>(a, st) : launch_spread<__nv_bfloat16, 2>(a, st));
+  return report_cuda(width == 16 ? launch_spread<float, 16>(a, st) : launch_spread<float, 4>(a, st));
 }
 
 int pgc_join(int32_t dtype, int64_t tokens, int32_t k, int64_t d, const void *rows_in, int64_t ld, int64_t rows,
@@ -579,7 +593,10 @@ int pgc_join(int32_t dtype, int64_t tokens, int32_t k, int64_t d, const void *ro
   a.k = k; a.d = (int)d;
   const cudaStream_t st = (cudaStream_t)stream;
   const int width = width_of({(uintptr_t)rows_in, (uintptr_t)out, (uintptr_t)ld * size, (uintptr_t)out_ld * size});
-  return report_cuda(by_width(dtype, width, Join{a, st}));
+  if (dtype == PGC_BF16)
+    return report_cuda(width == 16 ? launch_join<__nv_bfloat16, 16>(a, st)
+                       : width == 4 ? launch_join<__nv_bfloat16, 4>(a, st) : launch_join<__nv_bfloat16, 2>(a, st));
+  return report_cuda(width == 16 ? launch_join<float, 16>(a, st) : launch_join<float, 4>(a, st));
 }
 
 int pgc_join_grad(int32_t dtype, int64_t tokens, int32_t k, int64_t d, const void *dy, int64_t dy_ld, const void *rows_in,
@@ -599,8 +616,11 @@ int pgc_join_grad(int32_t dtype, int64_t tokens, int32_t k, int64_t d, const voi
   a.T = tokens; a.rows = rows; a.ldx = ld; a.ldy = dy_ld; a.ldo = drows_ld; a.k = k; a.d = (int)d;
   const cudaStream_t st = (cudaStream_t)stream;
   const int width = width_of({(uintptr_t)dy, (uintptr_t)rows_in, (uintptr_t)drows, (uintptr_t)dy_ld * size,
-                              (uintptr_t)ld * size, (uintptr_t)drows_ld * size});
-  return report_cuda(by_width(dtype, width, JoinGrad{a, st}));
+                            (uintptr_t)ld * size, (uintptr_t)drows_ld * size});
+  if (dtype == PGC_BF16)
+    return report_cuda(width == 16 ? launch_join_grad<__nv_bfloat16, 16>(a, st)
+                       : width == 4 ? launch_join_grad<__nv_bfloat16, 4>(a, st) : launch_join_grad<__nv_bfloat16, 2>(a, st));
+  return report_cuda(width == 16 ? launch_join_grad<float, 16>(a, st) : launch_join_grad<float, 4>(a, st));
 }
 
 }  // extern "C"
