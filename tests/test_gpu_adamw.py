@@ -330,3 +330,29 @@ def test_elements_beyond_32_bits(cuda, optim):
         assert (np.abs(on_host(p[s:e]) - q) <= 2.0 ** -8 * np.abs(q) + 1e-6).all()
     del p, g, opt
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [0.0, 1e-20, 1e-12, 1e-6])
+def test_small_gradients_and_eps(cuda, optim, bits, eps):
+    """Gradients down to squares that are no normal floats: where a v of 32 bits is not exact
+    (below 2^-126 a rounding is 2^-150 of itself, not of its size) its root's error is added."""
+    torch = cuda
+    r = np.random.default_rng(1)
+    n = 3000
+    g = (r.standard_normal(n) * 10.0 ** r.uniform(-22, -4, n)).astype(np.float32)
+    g[:5] = 1e-4
+    p = torch.full((n,), 0.5, device="cuda")
+    opt = optim.AdamW([p], lr=0.01, eps=eps, weight_decay=0.0, bits=bits, betas=(0.9, 0.99))
+    opt.step([torch.from_numpy(g).cuda()])
+    g = g.astype(np.float64)
+    v = 0.01 * g * g
+    tiny = np.minimum(3 * 2.0 ** -150 / np.maximum(v, 1e-300), 1.0)
+    with np.errstate(all="ignore"):
+        step = 0.01 * g / (np.abs(g) + eps)
+        # v rounded to 0: the quotient by eps alone
+        low = np.abs(0.01 * g / (np.sqrt(np.maximum(v - 3 * 2.0 ** -150, 0.0) / 0.01) + eps))
+        tol = np.abs(step) * (20 * U + tiny) + np.maximum(low - np.abs(step), 0.0) * (tiny > U) + 4 * U * 0.5
+    got = on_host(p)
+    sure = np.isfinite(low)
+    assert sure.sum() > n / 3 and (np.abs(got - (0.5 - step)) <= tol * 1.01)[sure].all()
