@@ -23,7 +23,7 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kUnroll = 4;            // 16-byte pieces a thread has in flight
 constexpr int kMaxCluster = 8;
 constexpr int kMostTop = 64;
-constexpr int kWarpTop = 16;          // alternatives of a row that a warp has
+constexpr int kWarpTop = 32;          // alternatives of a row that a warp has: lanes
 
 struct Scores {
   const void* x;
@@ -106,21 +106,6 @@ __device__ __forceinline__ void add_pieces(Part& o, const uint4 (&v)[U], float c
   split(add2(log[0], log[1]), lo, hi);
   o.w += lo + hi;
 }
-template <typename E, int G>
-__device__ __forceinline__ Part slice_part(const E* x, const Slice& s, int tid, float c) {
-  constexpr int N = Elem<E>::N;
-  Part o;
-  const int body = s.first + s.head, rest = body + s.pieces * N;
-  if (tid < s.head + (s.last - rest)) add_one(o, Elem<E>::get(x + (tid < s.head ? s.first + tid : rest + tid - s.head)), c);
-  const uint4* p = reinterpret_cast<const uint4*>(x + body);
-  for (int i = tid; i < s.pieces; i += G * kUnroll) {
-    uint4 v[kUnroll];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) v[u] = i + u * G < s.pieces ? load16(p + i + u * G) : no_piece(Elem<E>::kLowest);
-    add_pieces<E>(o, v, c);
-  }
-  return o;
-}
 __device__ __forceinline__ Part warp_merge(const Part& o, float c) {
   Part r;
   r.m = warp_max(o.m);
@@ -143,11 +128,11 @@ __device__ __forceinline__ void sync_group() {
 }
 
 // ---- the k largest ---------------------------------------------------------------
-// Every thread knows the largest of its elements.  The k-th largest of these, t, is
-// at most the k-th largest element, so only threads that have met t or more, about k of
-// them, hold alternatives: their pieces are read again (from the L2 cache, as a rule) and
-// what reaches t, a few more than k elements, is ranked.  Keys order by value and then
-// by the lower class; no two are equal.
+// Every lane knows the largest of its elements, and of up to eight parts of them.  The r-th largest
+// of a warp's 32, with r = k over the group's warps, is reached by r elements of this warp, the least of the warps'
+// such bounds by k of the row: only what reaches it can be among the k largest.  The parts that do, a few more
+// than k, are read again (from the L2 cache, as a rule), and what reaches the bound there is ranked.  Keys order
+// by value and then by the lower class; no two are equal.
 
 __device__ __forceinline__ Key key_of(float f, unsigned v) {
   const uint32_t b = __float_as_uint(f + 0.f);              // zeros of both signs are equal
@@ -162,26 +147,50 @@ __device__ __forceinline__ float value_of(Key q) {
 template <int G>
 struct Top {
   static constexpr int kKeys = G * 8 + kMostTop;            // the ones kept and a step of eight each
+  static constexpr int kParts = 8;
   static constexpr int kTop = G == 32 ? kWarpTop : kMostTop;
   Key key[kKeys];
   Key best[kTop];                                           // largest first, 0 where there is none
-  alignas(16) float most[G];
-  uint16_t hot[G];
+  alignas(16) float most[kParts * G];                       // by parts, then threads
+  uint16_t hot[kParts * G];
   Key red[G / 32];
+  float warp_bound[G / 32];
   float bound;
   int keys, hots;
 };
 
-// The k largest of sh.key[0 .. n) into sh.best, by all threads of the group.
+// The n-th largest of the lanes' values, n = 1 .. 32: they are sorted.
+__device__ __forceinline__ float warp_nth(float v, int n) {
+  const int lane = threadIdx.x % 32;
+#pragma unroll
+  for (int size = 2; size <= 32; size *= 2)
+#pragma unroll
+    for (int o = size / 2; o > 0; o /= 2) {
+      const float other = __shfl_xor_sync(0xffffffffu, v, o);
+      v = ((lane & o) == 0) == ((lane & size) == 0) ? fmaxf(v, other) : fminf(v, other);
+    }
+  return __shfl_sync(0xffffffffu, v, n - 1);
+}
 template <int G>
-__device__ __forceinline__ void rank_keys(Top<G>& sh, int n, int k, int tid) {
+__device__ __forceinline__ float least_bound(const Top<G>& sh) {
+  float bound = INFINITY;
+#pragma unroll
+  for (int w = 0; w < G / 32; ++w) bound = fminf(bound, sh.warp_bound[w]);
+  return bound;
+}
+
+// The k largest of n keys into sh.best, by all threads of the group: each one's rank, or, of more than two a
+// thread, one after another.
+template <int G>
+__device__ __forceinline__ void rank_keys(Top<G>& sh, const Key* keys, int n, int k, int tid) {
   if (tid < k) sh.best[tid] = 0;
   sync_group<G>();
   if (n <= 2 * G) {
     for (int i = tid; i < n; i += G) {
-      const Key mine = sh.key[i];
+      const Key mine = keys[i];
       int rank = 0;
-      for (int j = 0; j < n; ++j) rank += sh.key[j] > mine;
+#pragma unroll 4
+      for (int j = 0; j < n; ++j) rank += keys[j] > mine;
       if (rank < k) sh.best[rank] = mine;
     }
     sync_group<G>();
@@ -191,7 +200,7 @@ __device__ __forceinline__ void rank_keys(Top<G>& sh, int n, int k, int tid) {
   for (int j = 0; j < k; ++j) {
     Key most = 0;
     for (int i = tid; i < n; i += G) {
-      const Key q = sh.key[i];
+      const Key q = keys[i];
       if (q < before && q > most) most = q;
     }
 #pragma unroll
@@ -250,7 +259,7 @@ __device__ __noinline__ void top_in_steps(const E* x, Slice s, int tid, int k, T
     sync_group<G>();
     n = sh.keys;
     if (n > kMostTop) {
-      rank_keys<G>(sh, n, k, tid);
+      rank_keys<G>(sh, sh.key, n, k, tid);
       n = 0;
       for (int j = 0; j < k; ++j) n += sh.best[j] != 0;
       if (n == k) least = sh.best[k - 1];
@@ -260,13 +269,15 @@ __device__ __noinline__ void top_in_steps(const E* x, Slice s, int tid, int k, T
     }
     sync_group<G>();
   }
-  rank_keys<G>(sh, n, k, tid);
+  rank_keys<G>(sh, sh.key, n, k, tid);
 }
 
-// most: the thread's largest element.
+// The slice read again: the bound is the k-th largest of all the threads' largest elements, and only
+// threads that have met it, about k of them, hold alternatives.
 template <typename E, int G>
-__device__ __forceinline__ void slice_top(const E* x, const Slice& s, int tid, int k, float most, Top<G>& sh) {
+__device__ __noinline__ void top_again(const E* x, Slice s, int tid, int k, float most, Top<G>& sh) {
   constexpr int N = Elem<E>::N;
+  sync_group<G>();
   sh.most[tid] = most;
   if (tid == 0) sh.keys = sh.hots = 0;
   sync_group<G>();
@@ -318,7 +329,112 @@ __device__ __forceinline__ void slice_top(const E* x, const Slice& s, int tid, i
   }
   sync_group<G>();
   const int n = sh.keys;
-  if (n <= Top<G>::kKeys) rank_keys<G>(sh, n, k, tid);
+  if (n <= Top<G>::kKeys) rank_keys<G>(sh, sh.key, n, k, tid);
+  else top_in_steps<E, G>(x, s, tid, k, sh);
+}
+
+// Groups of pieces in a part.
+template <int G>
+__device__ __forceinline__ int groups_of_part(const Slice& s) {
+  return ((s.pieces + G * kUnroll - 1) / (G * kUnroll) + Top<G>::kParts - 1) / Top<G>::kParts;
+}
+// A warp's row whose pieces stay in registers until their bound is known.
+template <int G>
+__device__ __forceinline__ bool at_once(const Slice& s) { return G == 32 && s.pieces > 0 && s.pieces <= G * kUnroll; }
+template <int G>
+__device__ __forceinline__ void push(float f, int v, float bound, Top<G>& sh) {
+  if (!(f >= bound)) return;
+  const int at = atomicAdd(&sh.keys, 1);
+  if (at < Top<G>::kKeys) sh.key[at] = key_of(f, (unsigned)v);
+}
+template <typename E, int G>
+__device__ __forceinline__ void push_piece(const uint4& piece, int first, float bound, Top<G>& sh) {
+  float f[8];
+  each<E>(piece, f);
+#pragma unroll
+  for (int j = 0; j < Elem<E>::N; ++j) push(f[j], first + j, bound, sh);
+}
+// A slice's sums in one pass, its parts' largest elements and the warps' bounds.
+template <typename E, int G>
+__device__ __forceinline__ Part scan(const E* x, const Slice& s, int tid, float c, int k, Top<G>& sh) {
+  constexpr int N = Elem<E>::N;
+  Part o;
+  const int body = s.first + s.head, rest = body + s.pieces * N;
+  if (tid < s.head + (s.last - rest)) add_one(o, Elem<E>::get(x + (tid < s.head ? s.first + tid : rest + tid - s.head)), c);
+  const uint4* p = reinterpret_cast<const uint4*>(x + body);
+  const int groups = groups_of_part<G>(s);
+  float most = -INFINITY;
+  uint4 v[kUnroll];
+  for (int i0 = 0, part = 0, left = groups; i0 < s.pieces; i0 += G * kUnroll) {
+    const int i = i0 + tid;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) v[u] = i + u * G < s.pieces ? load16(p + i + u * G) : no_piece(Elem<E>::kLowest);
+    add_pieces<E>(o, v, c);
+    if (!k || at_once<G>(s)) continue;
+    most = fmaxf(most, Elem<E>::top(v));
+    if (--left == 0 || i0 + G * kUnroll >= s.pieces) {
+      sh.most[part++ * G + tid] = most;
+      most = -INFINITY;
+      left = groups;
+    }
+  }
+  if (k) {
+    const float bound = warp_nth(o.m, G == 32 ? k : (k + G / 32 - 1) / (G / 32));
+    if (tid % 32 == 0) sh.warp_bound[tid / 32] = bound;
+    if (tid == 0) sh.keys = sh.hots = 0;
+    if (G == 32) __syncwarp();
+    if (at_once<G>(s) && bound > -INFINITY) {
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const uint4 one[1] = {v[u]};
+        if (tid + u * G < s.pieces && Elem<E>::top(one) >= bound) push_piece<E, G>(v[u], body + (tid + u * G) * N, bound, sh);
+      }
+    }
+  }
+  return o;
+}
+// The k largest, after scan and a barrier behind it.
+template <typename E, int G>
+__device__ __forceinline__ void scan_top(const E* x, const Slice& s, int tid, int k, const Part& o, Top<G>& sh) {
+  constexpr int N = Elem<E>::N;
+  const float bound = least_bound(sh);
+  if (bound == -INFINITY) {
+    top_again<E, G>(x, s, tid, k, o.m, sh);
+    return;
+  }
+  const int body = s.first + s.head, rest = body + s.pieces * N, groups = groups_of_part<G>(s);
+  if (o.m >= bound) {
+    const int parts = s.pieces && !at_once<G>(s) ? ((s.pieces + G * kUnroll - 1) / (G * kUnroll) + groups - 1) / groups : 0;
+    for (int q = 0; q < parts; ++q)
+      if (sh.most[q * G + tid] >= bound) sh.hot[atomicAdd(&sh.hots, 1)] = (uint16_t)(q * G + tid);
+    if (tid < s.head + (s.last - rest)) {
+      const int v = tid < s.head ? s.first + tid : rest + tid - s.head;
+      push(Elem<E>::get(x + v), v, bound, sh);
+    }
+  }
+  sync_group<G>();
+  const unsigned per = groups * kUnroll, items = per * (unsigned)sh.hots;
+  const uint4* p = reinterpret_cast<const uint4*>(x + body);
+  for (unsigned i = tid; i < items; i += G * kUnroll) {
+    uint4 v[kUnroll];
+    int at[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const unsigned item = i + u * G, h = item / per;
+      at[u] = s.pieces;
+      if (item < items) at[u] = (int)((sh.hot[h] / G * per + (item - h * per)) * G + sh.hot[h] % G);
+      if (at[u] < s.pieces) v[u] = load16(p + at[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      if (at[u] >= s.pieces) continue;
+      const uint4 one[1] = {v[u]};
+      if (Elem<E>::top(one) >= bound) push_piece<E, G>(v[u], body + at[u] * N, bound, sh);
+    }
+  }
+  sync_group<G>();
+  const int n = sh.keys;
+  if (n <= Top<G>::kKeys) rank_keys<G>(sh, sh.key, n, k, tid);
   else top_in_steps<E, G>(x, s, tid, k, sh);
 }
 
@@ -371,9 +487,11 @@ __device__ __noinline__ float3 part_extreme(const E* x, Slice s, int tid, float 
 }
 
 template <typename E, int G>
-__device__ __forceinline__ float3 row_part(const E* x, const Slice& s, int tid, const Scores& a, Part& o, float4* red) {
-  o = slice_part<E, G>(x, s, tid, a.c);
+__device__ __forceinline__ float3 row_part(const E* x, const Slice& s, int tid, const Scores& a, Part& o, Shared<G>& sh) {
+  float4* red = sh.part;
+  o = scan<E, G>(x, s, tid, a.c, a.k, sh.top);
   Part q = warp_merge(o, a.c);
+  if (G == 32) __syncwarp();
   if (G > 32) {
     const int lane = tid % 32;
     if (lane == 0) red[tid / 32] = make_float4(q.m, q.M, q.s, q.w);
@@ -420,7 +538,7 @@ __device__ __forceinline__ void write_none(const Scores& a, int64_t t, int tid) 
 
 // A row per warp (G = 32), CTA or cluster of CTAs.
 template <typename E, int G>
-__global__ void __launch_bounds__(kThreads) scores_kernel(Scores a) {
+__global__ void __launch_bounds__(kThreads, 5) scores_kernel(Scores a) {
   extern __shared__ __align__(16) unsigned char raw[];
   Shared<G>& sh = reinterpret_cast<Shared<G>*>(raw)[G == 32 ? threadIdx.x / 32 : 0];
   const int rank = G == 32 ? 0 : cluster_rank(), ranks = G == 32 ? 1 : cluster_ranks();
@@ -438,8 +556,8 @@ __global__ void __launch_bounds__(kThreads) scores_kernel(Scores a) {
   const float xy = a.y && y < a.V ? Elem<E>::get(x + y) : NAN;
   const Slice s = slice_of(x, a.V, rank, ranks);
   Part mine;
-  float3 q = row_part<E, G>(x, s, tid, a, mine, sh.part);
-  if (a.k) slice_top<E, G>(x, s, tid, a.k, mine.m, sh.top);
+  float3 q = row_part<E, G>(x, s, tid, a, mine, sh);
+  if (a.k) scan_top<E, G>(x, s, tid, a.k, mine, sh.top);
   if (ranks == 1) {
     write_row(a, t, finish(q), xy, sh.top.best, tid);
     return;
@@ -476,9 +594,102 @@ __global__ void __launch_bounds__(kThreads) scores_kernel(Scores a) {
   if (a.k) {
     for (int i = tid; i < ranks * a.k; i += G) sh.top.key[i] = all.key[i];
     __syncthreads();
-    rank_keys<G>(sh.top, ranks * a.k, a.k, tid);
+    rank_keys<G>(sh.top, sh.top.key, ranks * a.k, a.k, tid);
   }
   write_row(a, t, finish(make_float3(m, sum, log)), xy, sh.top.best, tid);
+}
+
+// ---- short rows --------------------------------------------------------------------
+// Rows of up to L R classes in the registers of L lanes, so that a warp has 32 / L rows at once:
+// what a row costs there is its own instructions, not its bytes.  Elements are single ones, or (P = 2: bf16
+// rows of even length and pitch that start on 4 bytes) two neighbours.
+template <int L, int P>
+__device__ __forceinline__ int short_at(int l, int j) { return P * (l + j / P * L) + j % P; }
+template <typename E, int L, int R, int P>
+__device__ __forceinline__ void short_load(const E* x, int l, int V, bool taken, float (&v)[R]) {
+#pragma unroll
+  for (int j = 0; j < R; j += P) {
+    const int e = short_at<L, P>(l, j);
+    if constexpr (P == 2) {
+      const uint32_t w = taken && e < V ? *reinterpret_cast<const uint32_t*>(x + e) : Elem<E>::kLowest;
+      v[j] = __uint_as_float(w << 16);
+      v[j + 1] = __uint_as_float(w & 0xffff0000u);
+    } else {
+      v[j] = taken && e < V ? Elem<E>::get(x + e) : -INFINITY;
+    }
+  }
+}
+template <int L>
+__device__ __forceinline__ float group_add(float v) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+template <typename E, int L, int R, int P>
+__global__ void __launch_bounds__(kThreads) short_scores_kernel(Scores a) {
+  const int lane = threadIdx.x % 32, l = lane % L;
+  const int64_t t = (blockIdx.x * (int64_t)kWarps + threadIdx.x / 32) * (32 / L) + lane / L;
+  const int32_t y = t < a.T ? a.y ? a.y[t] : 0 : -1;
+  const bool taken = y >= 0;
+  const E* x = static_cast<const E*>(a.x) + t * a.ld;
+  float v[R];
+  short_load<E, L, R, P>(x, l, a.V, taken, v);
+  const float xy = taken && a.y && y < a.V ? Elem<E>::get(x + y) : NAN;
+  float m = v[0];
+#pragma unroll
+  for (int j = 1; j < R; ++j) m = fmaxf(m, v[j]);
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  float sum = 0.f, log = 0.f;
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    const float z = (v[j] - m) * a.c, e = ex2(z);
+    sum += e;
+    log += times_log(e, z);
+  }
+  sum = group_add<L>(sum);
+  log = group_add<L>(log);
+  const float3 r = taken ? finish(make_float3(m, sum, log)) : make_float3(0.f, 0.f, 0.f);
+  if (l == 0 && t < a.T) {
+    if (a.logp) a.logp[t] = taken ? (xy - r.x) * a.inv_tau - r.y : 0.f;
+    a.entropy[t] = r.z;
+    a.stats[t] = make_float2(r.x, r.y);
+  }
+  // one after another: the group's largest, of equal ones the lower class; L of them are written at once
+  int of = -1;
+  float q = -INFINITY;
+  for (int i = 0; i < a.k; ++i) {
+    float best = -INFINITY;
+    int at = INT32_MAX;
+#pragma unroll
+    for (int j = 0; j < R; ++j)
+      if (v[j] > best) {
+        best = v[j];
+        at = short_at<L, P>(l, j);
+      }
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) {
+      const float f = __shfl_xor_sync(0xffffffffu, best, o);
+      const int e = __shfl_xor_sync(0xffffffffu, at, o);
+      if (f > best || (f == best && e < at)) {
+        best = f;
+        at = e;
+      }
+    }
+    const bool any = best > -INFINITY;
+#pragma unroll
+    for (int j = 0; j < R; ++j)
+      if (any && short_at<L, P>(l, j) == at) v[j] = -INFINITY;
+    if (l == i % L) {
+      of = any ? at : -1;
+      q = any ? (best - r.x) * a.inv_tau - r.y : -INFINITY;
+    }
+    const int first = i / L * L;
+    if ((i % L == L - 1 || i == a.k - 1) && t < a.T && first + l <= i) {
+      a.top[t * a.k + first + l] = of;
+      a.top_logp[t * a.k + first + l] = q;
+    }
+  }
 }
 
 // ---- gradient ----------------------------------------------------------------------
@@ -537,6 +748,24 @@ __device__ __forceinline__ void slope_piece(const uint4& v, E* out, bool wide, c
   }
 }
 
+// What a row's derivatives ask for: zeros where they are 0, NaN where there is no gradient, or a slope.
+struct RowSlope {
+  bool filled;
+  float fill;
+  Slope r;
+};
+__device__ __forceinline__ RowSlope row_slope(const Scores& a, int64_t t, int32_t y, const float* dlogp, const float* dentropy) {
+  const float da = dlogp && y >= 0 ? dlogp[t] : 0.f, db = dentropy && y >= 0 ? dentropy[t] : 0.f;
+  const float2 st = a.stats[t];
+  const float H = db != 0.f ? a.entropy[t] : 0.f;
+  const bool none = da == 0.f && db == 0.f;
+  RowSlope q;
+  q.filled = none || isnan(da) || isnan(db) || isnan(st.y) || isnan(H) || (da != 0.f && y >= a.V);
+  q.fill = none ? 0.f : NAN;
+  q.r = slope_of(st, H, da, db, a.inv_tau, a.c, da != 0.f ? y : -1);
+  return q;
+}
+
 // A row, or one of its `parts`, per group: nothing is exchanged between them.  In place too: a thread
 // reads what it writes before it does, and the target's logit, which the thread of its piece writes again.
 template <typename E, int G>
@@ -550,17 +779,14 @@ __global__ void __launch_bounds__(kThreads) scores_grad_kernel(Scores a, int par
   const E* x = static_cast<const E*>(a.x) + t * a.ld;
   E* g = static_cast<E*>(a.g) + t * a.ldg;
   const Slice s = slice_of(x, a.V, rank, ranks);
-  const float da = dlogp && y >= 0 ? dlogp[t] : 0.f, db = dentropy && y >= 0 ? dentropy[t] : 0.f;
-  const float2 st = a.stats[t];
-  const float H = db != 0.f ? a.entropy[t] : 0.f;
-  const bool none = da == 0.f && db == 0.f;
-  if (none || isnan(da) || isnan(db) || isnan(st.y) || isnan(H) || (da != 0.f && y >= a.V)) {
-    slice_fill<E, G>(g, s.first, s.last, tid, none ? 0.f : NAN);
+  const RowSlope row = row_slope(a, t, y, dlogp, dentropy);
+  if (row.filled) {
+    slice_fill<E, G>(g, s.first, s.last, tid, row.fill);
     return;
   }
-  const int target = da != 0.f ? y : -1;
+  const Slope& r = row.r;
+  const int target = r.y;
   const float xy = target >= 0 ? Elem<E>::get(x + target) : 0.f;
-  const Slope r = slope_of(st, H, da, db, a.inv_tau, a.c, target);
   if (r.extreme) {
     for (unsigned v = s.first + tid; v < (unsigned)s.last; v += G)
       Elem<E>::put(g + v, slope_at(Elem<E>::get(x + v), (int)v == target, r));
@@ -584,6 +810,35 @@ __global__ void __launch_bounds__(kThreads) scores_grad_kernel(Scores a, int par
   }
   const int at = target - body;
   if (target >= 0 && at >= 0 && at < s.pieces * N && at / N % G == tid) Elem<E>::put(g + target, slope_at(xy, true, r));
+}
+
+template <typename E, int L, int R, int P>
+__global__ void __launch_bounds__(kThreads) short_scores_grad_kernel(Scores a, const float* dlogp, const float* dentropy) {
+  const int lane = threadIdx.x % 32, l = lane % L;
+  const int64_t t = (blockIdx.x * (int64_t)kWarps + threadIdx.x / 32) * (32 / L) + lane / L;
+  if (t >= a.T) return;
+  const int32_t y = a.y ? a.y[t] : 0;
+  const RowSlope row = row_slope(a, t, y, dlogp, dentropy);
+  E* g = static_cast<E*>(a.g) + t * a.ldg;
+  float v[R];
+  short_load<E, L, R, P>(static_cast<const E*>(a.x) + t * a.ld, l, a.V, !row.filled, v);
+  const bool words = reinterpret_cast<uintptr_t>(g) % 4 == 0;
+#pragma unroll
+  for (int j = 0; j < R; j += P) {
+    const int e = short_at<L, P>(l, j);
+    if (e >= a.V) continue;
+    float d[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) d[i] = row.filled ? row.fill : slope_at(v[j + i], e + i == row.r.y, row.r);
+    if constexpr (P == 2) {
+      if (words) {
+        *reinterpret_cast<uint32_t*>(g + e) = Elem<E>::two(pair(d[0], d[1]));
+        continue;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) Elem<E>::put(g + e + i, d[i]);
+  }
 }
 
 // ---- host --------------------------------------------------------------------
@@ -621,7 +876,7 @@ int sm_count() {
 // Rows as in the losses' streaming passes: a warp takes one up to 4 KB, or 24 KB
 // where there are rows for all warps; few long rows are split over a cluster while the SMs hold more CTAs and a part
 // stays above 4 KB.
-constexpr int64_t kWarpRowBytes = 4 * 1024, kWarpManyRowsBytes = 24 * 1024;
+constexpr int64_t kWarpRowBytes = 4 * 1024, kWarpManyRowsBytes = 24 * 1024, kWarpManyTopBytes = 72 * 1024;
 struct Shape {
   bool warp;
   int ranks;
@@ -629,7 +884,8 @@ struct Shape {
 };
 Shape shape_of(const pgc_logits* z, int k) {
   const int64_t bytes = z->classes * (z->dtype == PGC_BF16 ? 2 : 4), sms = sm_count();
-  Shape s{k <= kWarpTop && (bytes <= kWarpRowBytes || (bytes <= kWarpManyRowsBytes && z->rows >= 32 * sms)), 1, 0};
+  const int64_t many = k ? kWarpManyTopBytes : kWarpManyRowsBytes;
+  Shape s{k <= kWarpTop && (bytes <= kWarpRowBytes || (bytes <= many && z->rows >= 32 * sms)), 1, 0};
   if (s.warp) {
     s.grid = (unsigned)((z->rows + kWarps - 1) / kWarps);
     return s;
@@ -638,6 +894,53 @@ Shape shape_of(const pgc_logits* z, int k) {
   s.grid = (unsigned)(z->rows * s.ranks);
   return s;
 }
+
+// Rows of bf16 whose elements can be taken in pairs, and rows that are held in registers: up to 128
+// classes by 8 lanes, 256 by 16, 512 by 32 (fp32, and bf16 in pairs).
+bool in_pairs(const pgc_logits* z) { return z->classes % 2 == 0 && z->ld % 2 == 0 && (uintptr_t)z->x % 4 == 0; }
+bool short_rows(const pgc_logits* z) { return z->classes <= (z->dtype == PGC_F32 || in_pairs(z) ? 512 : 256); }
+unsigned short_grid(const pgc_logits* z) {
+  const int64_t rows = kWarps * (z->classes <= 128 ? 4 : z->classes <= 256 ? 2 : 1);
+  return (unsigned)((z->rows + rows - 1) / rows);
+}
+// f.template operator()<E, L, R, P>()
+template <typename F>
+cudaError_t by_width(const pgc_logits* z, F f) {
+  const int64_t V = z->classes;
+  if (z->dtype == PGC_F32) {
+    if (V <= 16) return f.template operator()<float, 8, 2, 1>();
+    if (V <= 64) return f.template operator()<float, 8, 8, 1>();
+    if (V <= 128) return f.template operator()<float, 8, 16, 1>();
+    if (V <= 256) return f.template operator()<float, 16, 16, 1>();
+    return f.template operator()<float, 32, 16, 1>();
+  }
+  using H = __nv_bfloat16;
+  const bool two = in_pairs(z);
+  if (V <= 16) return f.template operator()<H, 8, 2, 1>();
+  if (V <= 64) return two ? f.template operator()<H, 8, 8, 2>() : f.template operator()<H, 8, 8, 1>();
+  if (V <= 128) return two ? f.template operator()<H, 8, 16, 2>() : f.template operator()<H, 8, 16, 1>();
+  if (V <= 256) return two ? f.template operator()<H, 16, 16, 2>() : f.template operator()<H, 16, 16, 1>();
+  return f.template operator()<H, 32, 16, 2>();
+}
+struct ShortScores {
+  const pgc_logits* z;
+  Scores a;
+  cudaStream_t st;
+  template <typename E, int L, int R, int P> cudaError_t operator()() {
+    short_scores_kernel<E, L, R, P><<<short_grid(z), kThreads, 0, st>>>(a);
+    return cudaGetLastError();
+  }
+};
+struct ShortGrad {
+  const pgc_logits* z;
+  Scores a;
+  const float *dlogp, *dentropy;
+  cudaStream_t st;
+  template <typename E, int L, int R, int P> cudaError_t operator()() {
+    short_scores_grad_kernel<E, L, R, P><<<short_grid(z), kThreads, 0, st>>>(a, dlogp, dentropy);
+    return cudaGetLastError();
+  }
+};
 
 template <typename E>
 cudaError_t launch_scores(const Scores& a, const Shape& s, cudaStream_t st) {
@@ -691,6 +994,7 @@ int pgc_token_scores(const pgc_logits *z, int32_t k, float *logp, float *entropy
   a.k = k; a.logp = logp; a.entropy = entropy; a.top = top; a.top_logp = top_logp;
   a.stats = reinterpret_cast<float2*>(stats);
   const cudaStream_t st = (cudaStream_t)stream;
+  if (short_rows(z)) return report_cuda(by_width(z, ShortScores{z, a, st}));
   const Shape s = shape_of(z, k);
   return report_cuda(z->dtype == PGC_BF16 ? launch_scores<__nv_bfloat16>(a, s, st) : launch_scores<float>(a, s, st));
 }
@@ -706,6 +1010,7 @@ int pgc_token_scores_grad(const pgc_logits *z, const float *stats, const float *
   a.stats = reinterpret_cast<float2*>(const_cast<float*>(stats));
   a.entropy = const_cast<float*>(entropy);
   const cudaStream_t st = (cudaStream_t)stream;
+  if (short_rows(z)) return report_cuda(by_width(z, ShortGrad{z, a, dlogp, dentropy, st}));
   const Shape s = shape_of(z, 0);
   return report_cuda(z->dtype == PGC_BF16 ? launch_grad<__nv_bfloat16>(a, s, dlogp, dentropy, st)
                                           : launch_grad<float>(a, s, dlogp, dentropy, st));
