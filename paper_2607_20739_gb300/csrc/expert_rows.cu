@@ -73,6 +73,7 @@ __global__ void __launch_bounds__(kRouteThreads) count_kernel(Route a) {
   clear(count, a.E);
   __syncthreads();
   const int64_t first = (int64_t)blockIdx.x * a.per, last = min(first + a.per, (int64_t)a.n);
+#pragma unroll 4
   for (int64_t s = first + threadIdx.x; s < last; s += kRouteThreads) {
     const int e = expert_of(a, (int)s);
     if (e >= 0) atomicAdd(&count[e], 1);
@@ -81,41 +82,52 @@ __global__ void __launch_bounds__(kRouteThreads) count_kernel(Route a) {
   for (int e = threadIdx.x; e < a.E; e += kRouteThreads) a.counts[(int64_t)blockIdx.x * a.E + e] = count[e];
 }
 
+// counts[c][e] becomes what CTAs before c count, and counts[CTAs][e] what all do: 32 experts a CTA, CTAs
+// in sixteen parts, a warp each, whose counts stay in registers between their sum and their places.
+constexpr int kMostRouteCtas = 256, kPartCtas = kMostRouteCtas / kRouteWarps;
+__global__ void __launch_bounds__(kRouteThreads) prefix_kernel(Route a, int ctas) {
+  __shared__ int32_t sum[kRouteWarps][32];
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, e = blockIdx.x * 32 + lane;
+  const int per = (ctas + kRouteWarps - 1) / kRouteWarps, first = warp * per;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  int32_t c[kPartCtas], all = 0;
+#pragma unroll
+  for (int i = 0; i < kPartCtas; ++i) {
+    c[i] = i < per && first + i < ctas && e < a.E ? __ldcg(a.counts + (int64_t)(first + i) * a.E + e) : 0;
+    all += c[i];
+  }
+  sum[warp][lane] = all;
+  __syncthreads();
+  if (e >= a.E) return;
+  int32_t before = 0;
+  for (int w = 0; w < warp; ++w) before += sum[w][lane];
+#pragma unroll
+  for (int i = 0; i < kPartCtas; ++i)
+    if (i < per && first + i < ctas) {
+      a.counts[(int64_t)(first + i) * a.E + e] = before;
+      before += c[i];
+    }
+  if (warp == kRouteWarps - 1) a.counts[(int64_t)ctas * a.E + e] = before;
+}
+
 // kAlone: one CTA has all slots, and counts them itself.
 template <bool kAlone>
 __global__ void __launch_bounds__(kRouteThreads) place_kernel(Route a) {
   extern __shared__ int32_t next[];              // [kRouteWarps][E]: the row of a warp's next slot of an expert
-  __shared__ int32_t total[kMaxExperts], base[kMaxExperts];
+  __shared__ int32_t base[kMaxExperts];
   __shared__ int red[kRouteWarps];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int64_t cta = (int64_t)blockIdx.x * a.per, first = cta + (int64_t)warp * (a.per / kRouteWarps);
   const int64_t last = min(first + a.per / kRouteWarps, (int64_t)a.n);
   clear(next, kRouteWarps * a.E);
-  clear(total, a.E);
-  clear(base, a.E);
   __syncthreads();
+#pragma unroll 4
   for (int64_t s = first + lane; s < last; s += 32) {
     const int e = expert_of(a, (int)s);
     if (e >= 0) atomicAdd(&next[warp * a.E + e], 1);
   }
-  if (!kAlone) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    // counts of all CTAs, and of those before this one: as many threads to an expert as there are
-    const int groups = max(kRouteThreads / a.E, 1), group = threadIdx.x / a.E;
-    const int width = groups > 1 ? a.E : kRouteThreads;
-    if (group < groups)
-      for (int e = threadIdx.x - group * width; e < a.E; e += width) {
-        int all = 0, before = 0;
-#pragma unroll 8
-        for (int b = group; b < (int)gridDim.x; b += groups) {
-          const int c = __ldcg(a.counts + (int64_t)b * a.E + e);
-          all += c;
-          before += b < (int)blockIdx.x ? c : 0;
-        }
-        atomicAdd(&total[e], all);
-        atomicAdd(&base[e], before);
-      }
-  }
+  if (!kAlone) asm volatile("griddepcontrol.wait;" ::: "memory");
   __syncthreads();
   // first row of every expert; a thread has two consecutive ones
   const int e0 = 2 * threadIdx.x;
@@ -125,14 +137,14 @@ __global__ void __launch_bounds__(kRouteThreads) place_kernel(Route a) {
     if (kAlone)
       for (int w = 0; w < kRouteWarps; ++w) c[i] += next[w * a.E + e0 + i];
     else
-      c[i] = total[e0 + i];
+      c[i] = __ldcg(a.counts + (int64_t)gridDim.x * a.E + e0 + i);
   }
   int rows;
   int at = before_me(c[0] + c[1], red, &rows);
   for (int i = 0; i < 2; ++i) {
     if (e0 + i >= a.E) continue;
     if (blockIdx.x == 0) a.offsets[e0 + i] = at;
-    base[e0 + i] += at;
+    base[e0 + i] = at + (kAlone ? 0 : __ldcg(a.counts + (int64_t)blockIdx.x * a.E + e0 + i));
     at += c[i];
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) a.offsets[a.E] = rows;
@@ -146,9 +158,11 @@ __global__ void __launch_bounds__(kRouteThreads) place_kernel(Route a) {
     }
   }
   __syncthreads();
+  int ahead = first + lane < last ? expert_of(a, (int)(first + lane)) : -1;
   for (int64_t s0 = first; s0 < last; s0 += 32) {
     const int64_t s = s0 + lane;
-    const int e = s < last ? expert_of(a, (int)s) : -1;
+    const int e = ahead;
+    ahead = s + 32 < last ? expert_of(a, (int)s + 32) : -1;
     const unsigned same = __match_any_sync(0xffffffffu, e);
     int row = -1;
     if (e >= 0) row = next[warp * a.E + e] + __popc(same & ((1u << lane) - 1));
@@ -471,9 +485,12 @@ int sm_count() {
   return n;
 }
 
-// CTAs of a large sort: 1024 slots each at least.  Up to 8192 slots one CTA does it all.
-constexpr int kAloneSlots = 8192, kMostRouteCtas = 128;
-int route_ctas(int64_t n) { return (int)std::min<int64_t>((n + 1023) / 1024, kMostRouteCtas); }
+// CTAs of a sort: one does up to 2048 slots (2.7 us for 64 on the GPU, 12.7 for 8000, which three kernels take 6 for); above,
+// each has 1024 at least.  65536 x 8 of 256: 14.8 us, 34.2 where every CTA read all counts itself.
+constexpr int kAloneSlots = 2048;
+int route_ctas(int64_t n) {
+  return n <= kAloneSlots ? 1 : (int)std::min<int64_t>((n + 1023) / 1024, kMostRouteCtas);
+}
 
 // The pieces that all rows' starts allow.
 int width_of(std::initializer_list<uintptr_t> starts) {
@@ -519,8 +536,8 @@ extern "C" {
 int pgc_route_workspace(int64_t tokens, int32_t k, int32_t experts, int64_t *bytes) {
   if (!bytes || tokens < 0 || k < 1 || tokens > INT32_MAX / k || experts < 1) return PGC_EINVAL;
   if (experts > kMaxExperts || k > kMaxChoices) return PGC_ENOTSUP;
-  const int64_t n = tokens * k;
-  *bytes = n <= kAloneSlots ? 16 : (int64_t)route_ctas(n) * experts * 4;
+  const int64_t ctas = route_ctas(tokens * k);
+  *bytes = ctas == 1 ? 16 : (ctas + 1) * experts * 4;
   return PGC_OK;
 }
 
@@ -535,7 +552,7 @@ int pgc_route(int64_t tokens, int32_t k, int32_t experts, const int32_t *choice,
   if (workspace_bytes < need) return PGC_ESCRATCH;
   const int64_t n = tokens * k;
   const cudaStream_t st = (cudaStream_t)stream;
-  const int ctas = n <= kAloneSlots ? 1 : route_ctas(n), grain = 32 * kRouteWarps;
+  const int ctas = route_ctas(n), grain = 32 * kRouteWarps;
   const int64_t per = ((n + ctas - 1) / ctas + grain - 1) / grain * grain;
   const Route a{choice, place, slot, offsets, static_cast<int32_t*>(workspace), (int)n, experts, (int)per};
   const size_t smem = (size_t)kRouteWarps * experts * 4;
@@ -544,21 +561,23 @@ int pgc_route(int64_t tokens, int32_t k, int32_t experts, const int32_t *choice,
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRouteWarps * kMaxExperts * 4);
     if (e != cudaSuccess) return report_cuda(e);
   }
-  if (ctas > 1) {
-    count_kernel<<<ctas, kRouteThreads, 0, st>>>(a);
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return report_cuda(e);
-  }
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)ctas);
   cfg.blockDim = dim3(kRouteThreads);
-  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cfg.attrs = &attr;
-  cfg.numAttrs = ctas > 1 ? 1 : 0;
+  if (ctas > 1) {
+    count_kernel<<<ctas, kRouteThreads, 0, st>>>(a);
+    cudaError_t e = cudaGetLastError();
+    cfg.numAttrs = 1;
+    cfg.gridDim = dim3((unsigned)(experts + 31) / 32);
+    if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, prefix_kernel, a, ctas);
+    if (e != cudaSuccess) return report_cuda(e);
+  }
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.dynamicSmemBytes = smem;
   return report_cuda(cudaLaunchKernelEx(&cfg, kernel, a));
 }
 

@@ -264,3 +264,12 @@ def test_rows_beyond_32_bits(cuda, experts):
     assert abs(float(dw[-1, 0]) - float(want)) <= U * (d / 32 + 65) * float(want)
     del x, e, drows
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("T,k,E", [(2048, 1, 16), (2049, 1, 16), (256, 8, 9), (257, 8, 9), (70000, 4, 31), (300000, 1, 33), (65536, 5, 1024)])
+def test_route_of_sorted_and_blocked_choices(cuda, experts, T, k, E):
+    """Choices that keep one expert in long runs: CTAs that hold only a few of the experts."""
+    torch = cuda
+    c = (np.arange(T * k) * E // (T * k)).astype(np.int32).reshape(T, k)
+    for choice in (c, c[::-1].copy(), np.where(c % 3 == 1, -5, c).astype(np.int32)):
+        check_routes(experts.route(torch.from_numpy(choice).cuda(), E), choice, E)
