@@ -10,8 +10,9 @@ autograd refuses a backward pass over a graph that kept their older values.
 
 from __future__ import annotations
 
-import math
+import ctypes as C
 
+import numpy as np
 import torch
 
 from . import binding as B
@@ -78,7 +79,11 @@ class AdamW:
             raise ValueError("the number of steps must not be negative")
         self._device_step = torch.full((), t, dtype=torch.int64, device=self.device) if device_step and self.params else None
         self._t = t
+        self._shapes = [p.shape for p in self.params]
         self._table = (B.AdamWTensor * len(self.params))()
+        # the column of the gradients' addresses
+        self._grads = np.frombuffer(self._table, dtype=np.int64).reshape(-1, C.sizeof(B.AdamWTensor) // 8)[
+            :, B.AdamWTensor.grad.offset // 8] if self.params else None
         for i, p in enumerate(self.params):
             e = self._table[i]
             e.param, e.m, e.v, e.n = p.data_ptr(), self.m[i].data_ptr(), self.v[i].data_ptr(), p.numel()
@@ -125,10 +130,15 @@ class AdamW:
         dtype = next((g.dtype for g in grads if isinstance(g, torch.Tensor)), torch.float32)
         if dtype not in _TYPES:
             raise ValueError("gradients must be float32 or bfloat16")
-        device, table = self.device, self._table
-        for i, (g, p) in enumerate(zip(grads, self.params)):
-            if g is not None:
-                _vector(f"grads[{i}]", g, dtype, p.shape, device)
+        device, addresses = self.device, []
+        for g, shape in zip(grads, self._shapes):
+            if g is None:
+                addresses.append(0)
+                continue
+            # what _vector asks for, without a name: a step of few elements lasts as long as this loop
+            if not isinstance(g, torch.Tensor) or g.dtype is not dtype or g.shape != shape or g.device != device or not g.is_contiguous():
+                _vector(f"grads[{len(addresses)}]", g, dtype, shape, device)
+            addresses.append(g.data_ptr())
         lr_at = None
         if isinstance(self.lr, torch.Tensor):
             _vector("lr", self.lr, torch.float32, tuple(self.lr.shape), device)
@@ -141,18 +151,19 @@ class AdamW:
                 raise ValueError("grad_scale must have one element")
         if not self.params:
             return
-        for e, g in zip(table, grads):
-            e.grad = None if g is None else g.data_ptr()
-
+        self._grads[:] = addresses
         def call(st):
             if self._device_step is not None:
                 self._device_step.add_(1)
             a = B.AdamW(0.0 if lr_at is not None else self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay,
                         self._t + 1, _address(self._device_step), _address(lr_at), _address(grad_scale),
                         self.seed & 0xffffffff, _TYPES[self.params[0].dtype], _TYPES[dtype], self.bits)
-            B._check(B.lib.pgc_adamw_step(a, table, len(table), st), "pgc_adamw_step")
-        kept = [self.params, self.m, self.v, self.m_scale or [], self.v_scale or [], self.copies or [], grads,
-                [lr_at, grad_scale, self._device_step]]
-        _on(device, stream, [t for group in kept for t in group] if stream is not None else (), call)
+            B._check(B.lib.pgc_adamw_step(a, self._table, len(self._table), st), "pgc_adamw_step")
+        kept = ()
+        if stream is not None:
+            kept = [self.params, self.m, self.v, self.m_scale or [], self.v_scale or [], self.copies or [], grads,
+                    [lr_at, grad_scale, self._device_step]]
+            kept = [t for group in kept for t in group]
+        _on(device, stream, kept, call)
         self._t += 1
         torch.autograd.graph.increment_version(self.params if self.copies is None else self.params + self.copies)
