@@ -11,6 +11,7 @@ autograd refuses a backward pass over a graph that kept their older values.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 
 import numpy as np
 import torch
@@ -21,6 +22,9 @@ from ._tensors import _TYPES, _address, _on, _vector
 __all__ = ["AdamW"]
 
 BLOCK = 256            # elements with a common scale, of moments in 8 bits
+
+_dtype_of, _shape_of = operator.attrgetter("dtype"), operator.attrgetter("shape")
+_device_of, _is_contiguous, _address_of = torch.Tensor.get_device, torch.Tensor.is_contiguous, torch.Tensor.data_ptr
 
 
 def _list(name, tensors, params, dtype, shape_of=lambda p: tuple(p.shape)):
@@ -80,6 +84,7 @@ class AdamW:
         self._device_step = torch.full((), t, dtype=torch.int64, device=self.device) if device_step and self.params else None
         self._t = t
         self._shapes = [p.shape for p in self.params]
+        self._devices = [p.get_device() for p in self.params]
         self._table = (B.AdamWTensor * len(self.params))()
         # the column of the gradients' addresses
         self._grads = np.frombuffer(self._table, dtype=np.int64).reshape(-1, C.sizeof(B.AdamWTensor) // 8)[
@@ -120,6 +125,25 @@ class AdamW:
             s["m_scale"], s["v_scale"] = self.m_scale, self.v_scale
         return s
 
+    def _addresses(self, grads):
+        """The gradients' type and addresses, 0 for None; refuses what does not go with the parameters."""
+        # A step of few elements lasts as long as this: five passes of C over the list (0.25 us a tensor), and the
+        # loop that finds what is wrong only where something is.
+        try:
+            kinds = set(map(_dtype_of, grads))
+            if len(kinds) == 1 and kinds <= _TYPES.keys() and list(map(_device_of, grads)) == self._devices and \
+                    list(map(_shape_of, grads)) == self._shapes and all(map(_is_contiguous, grads)):
+                return kinds.pop(), np.fromiter(map(_address_of, grads), np.int64, len(grads))
+        except (TypeError, AttributeError):
+            pass
+        dtype = next((g.dtype for g in grads if isinstance(g, torch.Tensor)), torch.float32)
+        if dtype not in _TYPES:
+            raise ValueError("gradients must be float32 or bfloat16")
+        for i, (g, shape) in enumerate(zip(grads, self._shapes)):
+            if g is not None:
+                _vector(f"grads[{i}]", g, dtype, shape, self.device)
+        return dtype, [0 if g is None else g.data_ptr() for g in grads]
+
     def step(self, grads, *, grad_scale=None, stream=None):
         """One step.  grads: a tensor shaped as each parameter (float32 or bfloat16, one type), or None for a
         parameter that stays as it is.  grad_scale: factor of the gradients, a float32 tensor
@@ -127,18 +151,8 @@ class AdamW:
         grads = list(grads)
         if len(grads) != len(self.params):
             raise ValueError(f"grads must have {len(self.params)} tensors, not {len(grads)}")
-        dtype = next((g.dtype for g in grads if isinstance(g, torch.Tensor)), torch.float32)
-        if dtype not in _TYPES:
-            raise ValueError("gradients must be float32 or bfloat16")
-        device, addresses = self.device, []
-        for g, shape in zip(grads, self._shapes):
-            if g is None:
-                addresses.append(0)
-                continue
-            # what _vector asks for, without a name: a step of few elements lasts as long as this loop
-            if not isinstance(g, torch.Tensor) or g.dtype is not dtype or g.shape != shape or g.device != device or not g.is_contiguous():
-                _vector(f"grads[{len(addresses)}]", g, dtype, shape, device)
-            addresses.append(g.data_ptr())
+        dtype, addresses = self._addresses(grads)
+        device = self.device
         lr_at = None
         if isinstance(self.lr, torch.Tensor):
             _vector("lr", self.lr, torch.float32, tuple(self.lr.shape), device)
@@ -152,6 +166,7 @@ class AdamW:
         if not self.params:
             return
         self._grads[:] = addresses
+
         def call(st):
             if self._device_step is not None:
                 self._device_step.add_(1)
