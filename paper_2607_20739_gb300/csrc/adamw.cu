@@ -543,20 +543,24 @@ bool dtype_ok(int32_t d) { return d == PGC_F32 || d == PGC_BF16; }
 // Elements of a tensor at most: the blocks of all tensors of a launch are counted in 32 bits.
 constexpr int64_t kMostElements = int64_t(1) << 38;
 
+// Whether all of the addresses are multiples of `bytes`, a power of two.
+template <typename... T>
+bool multiples(uintptr_t bytes, const T*... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) & (bytes - 1)) == 0; }
+
 int check(const pgc_adamw& s, const pgc_adamw_tensor& t) {
   if (t.n < 0 || t.n > kMostElements) return PGC_EINVAL;
-  const uintptr_t p = s.param_dtype == PGC_BF16 ? 2 : 4, g = s.grad_dtype == PGC_BF16 ? 2 : 4, st = s.bits == 8 ? 1 : 4;
-  if ((uintptr_t)t.param % p || (uintptr_t)t.grad % g || (uintptr_t)t.copy % 2 || (uintptr_t)t.m % st || (uintptr_t)t.v % st ||
-      (uintptr_t)t.m_scale % 4 || (uintptr_t)t.v_scale % 4)
+  if (!multiples(s.param_dtype == PGC_BF16 ? 2 : 4, t.param) || !multiples(s.grad_dtype == PGC_BF16 ? 2 : 4, t.grad) ||
+      !multiples(2, t.copy) || !multiples(s.bits == 8 ? 1 : 4, t.m, t.v) || !multiples(4, t.m_scale, t.v_scale))
     return PGC_EINVAL;
   if (!t.n || !t.grad) return PGC_OK;
   return !t.param || !t.m || !t.v || (s.bits == 8 && (!t.m_scale || !t.v_scale)) ? PGC_EINVAL : PGC_OK;
 }
 
-bool in_fours(const pgc_adamw& s, const pgc_adamw_tensor& t) {
-  const uintptr_t p = s.param_dtype == PGC_BF16 && s.bits == 32 ? 8 : 16, g = s.grad_dtype == PGC_BF16 && s.bits == 32 ? 8 : 16, st = 16;
-  return (uintptr_t)t.param % p == 0 && (uintptr_t)t.grad % g == 0 && (uintptr_t)t.copy % 8 == 0 && (uintptr_t)t.m % st == 0 &&
-         (uintptr_t)t.v % st == 0;
+// 16 bytes of every array at once: with 32-bit moments four elements, so that bf16 may start on 8.
+bool at_once(const pgc_adamw& s, const pgc_adamw_tensor& t) {
+  const uintptr_t half = s.bits == 32 ? 8 : 16;
+  return multiples(s.param_dtype == PGC_BF16 ? half : 16, t.param) && multiples(s.grad_dtype == PGC_BF16 ? half : 16, t.grad) &&
+         multiples(8, t.copy) && multiples(16, t.m, t.v);
 }
 
 }  // namespace
@@ -601,7 +605,7 @@ extern "C" int pgc_adamw_step(const pgc_adamw *s, const pgc_adamw_tensor *tensor
     }
     if (!blocks) continue;
     const pgc_adamw_tensor& q = tensors[i];
-    a.t[a.count] = Tensor{q.param, q.grad, static_cast<__nv_bfloat16*>(q.copy), q.m, q.v, q.m_scale, q.v_scale, in_fours(*s, q) ? q.n : q.n | INT64_MIN};
+    a.t[a.count] = Tensor{q.param, q.grad, static_cast<__nv_bfloat16*>(q.copy), q.m, q.v, q.m_scale, q.v_scale, at_once(*s, q) ? q.n : q.n | INT64_MIN};
     a.ordinal[a.count] = (uint32_t)i;
     a.first[a.count + 1] = a.first[a.count] + (uint32_t)blocks;
     ++a.count;
