@@ -23,7 +23,6 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kUnroll = 4;            // 16-byte pieces a thread has in flight
 constexpr int kMaxCluster = 8;
 constexpr int kMostTop = 64;
-constexpr int kWarpTop = 32;          // alternatives of a row that a warp has: lanes
 
 struct Scores {
   const void* x;
@@ -148,9 +147,8 @@ template <int G>
 struct Top {
   static constexpr int kKeys = G * 8 + kMostTop;            // the ones kept and a step of eight each
   static constexpr int kParts = 8;
-  static constexpr int kTop = G == 32 ? kWarpTop : kMostTop;
   Key key[kKeys];
-  Key best[kTop];                                           // largest first, 0 where there is none
+  Key best[kMostTop];                                          // largest first, 0 where there is none
   alignas(16) float most[kParts * G];                       // by parts, then threads
   uint16_t hot[kParts * G];
   Key red[G / 32];
@@ -179,13 +177,20 @@ __device__ __forceinline__ float least_bound(const Top<G>& sh) {
   return bound;
 }
 
+// f(j) for j = 0 .. n - 1, n up to 64: a thread each, or two of a warp.
+template <int G, typename F>
+__device__ __forceinline__ void for_top(int n, int tid, F f) {
+  if (tid < n) f(tid);
+  if (G == 32 && tid + 32 < n) f(tid + 32);
+}
+
 // The k largest of n keys into sh.best, by all threads of the group: each one's rank, or, of more than two a
-// thread, one after another.
+// thread of a CTA, one after another.
 template <int G>
 __device__ __forceinline__ void rank_keys(Top<G>& sh, const Key* keys, int n, int k, int tid) {
-  if (tid < k) sh.best[tid] = 0;
+  for_top<G>(k, tid, [&](int j) { sh.best[j] = 0; });
   sync_group<G>();
-  if (n <= 2 * G) {
+  if (n <= (G == 32 ? Top<G>::kKeys : 2 * G)) {
     for (int i = tid; i < n; i += G) {
       const Key mine = keys[i];
       int rank = 0;
@@ -264,7 +269,7 @@ __device__ __noinline__ void top_in_steps(const E* x, Slice s, int tid, int k, T
       for (int j = 0; j < k; ++j) n += sh.best[j] != 0;
       if (n == k) least = sh.best[k - 1];
       sync_group<G>();
-      if (tid < n) sh.key[tid] = sh.best[tid];
+      for_top<G>(n, tid, [&](int j) { sh.key[j] = sh.best[j]; });
       if (tid == 0) sh.keys = n;
     }
     sync_group<G>();
@@ -288,7 +293,7 @@ __device__ __noinline__ void top_again(const E* x, Slice s, int tid, int k, floa
     rank += (o.x > most || (o.x == most && i < tid)) + (o.y > most || (o.y == most && i + 1 < tid)) +
             (o.z > most || (o.z == most && i + 2 < tid)) + (o.w > most || (o.w == most && i + 3 < tid));
   }
-  if (rank == k - 1) sh.bound = most;
+  if (rank == k - 1 || (k > G && tid == 0)) sh.bound = k > G ? -INFINITY : most;
   sync_group<G>();
   const float bound = sh.bound;
   auto push = [&](float f, int v) {
@@ -355,7 +360,8 @@ __device__ __forceinline__ void push_piece(const uint4& piece, int first, float 
   for (int j = 0; j < Elem<E>::N; ++j) push(f[j], first + j, bound, sh);
 }
 // A slice's sums in one pass, its parts' largest elements and the warps' bounds.
-template <typename E, int G>
+// kMany: more alternatives than a warp has lanes.
+template <typename E, int G, bool kMany>
 __device__ __forceinline__ Part scan(const E* x, const Slice& s, int tid, float c, int k, Top<G>& sh) {
   constexpr int N = Elem<E>::N;
   Part o;
@@ -363,13 +369,20 @@ __device__ __forceinline__ Part scan(const E* x, const Slice& s, int tid, float 
   if (tid < s.head + (s.last - rest)) add_one(o, Elem<E>::get(x + (tid < s.head ? s.first + tid : rest + tid - s.head)), c);
   const uint4* p = reinterpret_cast<const uint4*>(x + body);
   const int groups = groups_of_part<G>(s);
-  float most = -INFINITY;
+  float most = -INFINITY, halves[2] = {-INFINITY, -INFINITY};
   uint4 v[kUnroll];
   for (int i0 = 0, part = 0, left = groups; i0 < s.pieces; i0 += G * kUnroll) {
     const int i = i0 + tid;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) v[u] = i + u * G < s.pieces ? load16(p + i + u * G) : no_piece(Elem<E>::kLowest);
     add_pieces<E>(o, v, c);
+    if (kMany) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint4 half[kUnroll / 2] = {v[h * kUnroll / 2], v[h * kUnroll / 2 + 1]};
+        halves[h] = fmaxf(halves[h], Elem<E>::top(half));
+      }
+    }
     if (!k || at_once<G>(s)) continue;
     most = fmaxf(most, Elem<E>::top(v));
     if (--left == 0 || i0 + G * kUnroll >= s.pieces) {
@@ -379,7 +392,8 @@ __device__ __forceinline__ Part scan(const E* x, const Slice& s, int tid, float 
     }
   }
   if (k) {
-    const float bound = warp_nth(o.m, G == 32 ? k : (k + G / 32 - 1) / (G / 32));
+    // a warp that has a whole row: k of its lanes, or half as many that have met it in both halves of their pieces
+    const float bound = kMany ? warp_nth(fminf(halves[0], halves[1]), (k + 1) / 2) : warp_nth(o.m, (k + G / 32 - 1) / (G / 32));
     if (tid % 32 == 0) sh.warp_bound[tid / 32] = bound;
     if (tid == 0) sh.keys = sh.hots = 0;
     if (G == 32) __syncwarp();
@@ -486,10 +500,10 @@ __device__ __noinline__ float3 part_extreme(const E* x, Slice s, int tid, float 
   return make_float3(m, sum, log);
 }
 
-template <typename E, int G>
+template <typename E, int G, bool kMany>
 __device__ __forceinline__ float3 row_part(const E* x, const Slice& s, int tid, const Scores& a, Part& o, Shared<G>& sh) {
   float4* red = sh.part;
-  o = scan<E, G>(x, s, tid, a.c, a.k, sh.top);
+  o = scan<E, G, kMany>(x, s, tid, a.c, a.k, sh.top);
   Part q = warp_merge(o, a.c);
   if (G == 32) __syncwarp();
   if (G > 32) {
@@ -514,22 +528,24 @@ __device__ __forceinline__ float3 finish(const float3& q) {
   return make_float3(q.x, logf(q.y), logf(q.y) - kLn2 * (q.z / q.y));
 }
 // Row t's results, by lane `tid` of the threads that have them all.
+template <int G>
 __device__ __forceinline__ void write_row(const Scores& a, int64_t t, float3 r, float xy, const Key* best, int tid) {
-  if (tid < a.k) {
-    const Key q = best[tid];
-    a.top[t * a.k + tid] = q ? class_of(q) : -1;
-    a.top_logp[t * a.k + tid] = q ? (value_of(q) - r.x) * a.inv_tau - r.y : -INFINITY;
-  }
+  for_top<G>(a.k, tid, [&](int j) {
+    const Key q = best[j];
+    a.top[t * a.k + j] = q ? class_of(q) : -1;
+    a.top_logp[t * a.k + j] = q ? (value_of(q) - r.x) * a.inv_tau - r.y : -INFINITY;
+  });
   if (tid) return;
   if (a.logp) a.logp[t] = (xy - r.x) * a.inv_tau - r.y;
   a.entropy[t] = r.z;
   a.stats[t] = make_float2(r.x, r.y);
 }
+template <int G>
 __device__ __forceinline__ void write_none(const Scores& a, int64_t t, int tid) {
-  if (tid < a.k) {
-    a.top[t * a.k + tid] = -1;
-    a.top_logp[t * a.k + tid] = -INFINITY;
-  }
+  for_top<G>(a.k, tid, [&](int j) {
+    a.top[t * a.k + j] = -1;
+    a.top_logp[t * a.k + j] = -INFINITY;
+  });
   if (tid) return;
   if (a.logp) a.logp[t] = 0.f;
   a.entropy[t] = 0.f;
@@ -537,8 +553,8 @@ __device__ __forceinline__ void write_none(const Scores& a, int64_t t, int tid) 
 }
 
 // A row per warp (G = 32), CTA or cluster of CTAs.
-template <typename E, int G>
-__global__ void __launch_bounds__(kThreads, 5) scores_kernel(Scores a) {
+template <typename E, int G, bool kMany>
+__global__ void __launch_bounds__(kThreads, G == 32 && sizeof(E) == 4 ? 4 : 5) scores_kernel(Scores a) {
   extern __shared__ __align__(16) unsigned char raw[];
   Shared<G>& sh = reinterpret_cast<Shared<G>*>(raw)[G == 32 ? threadIdx.x / 32 : 0];
   const int rank = G == 32 ? 0 : cluster_rank(), ranks = G == 32 ? 1 : cluster_ranks();
@@ -547,7 +563,7 @@ __global__ void __launch_bounds__(kThreads, 5) scores_kernel(Scores a) {
   if (t >= a.T) return;
   const int32_t y = a.y ? a.y[t] : 0;
   if (y < 0) {
-    if (rank == 0) write_none(a, t, tid);
+    if (rank == 0) write_none<G>(a, t, tid);
     return;
   }
   // a CTA's shared memory may be written by another one of its cluster only once it runs
@@ -556,10 +572,10 @@ __global__ void __launch_bounds__(kThreads, 5) scores_kernel(Scores a) {
   const float xy = a.y && y < a.V ? Elem<E>::get(x + y) : NAN;
   const Slice s = slice_of(x, a.V, rank, ranks);
   Part mine;
-  float3 q = row_part<E, G>(x, s, tid, a, mine, sh);
+  float3 q = row_part<E, G, kMany>(x, s, tid, a, mine, sh);
   if (a.k) scan_top<E, G>(x, s, tid, a.k, mine, sh.top);
   if (ranks == 1) {
-    write_row(a, t, finish(q), xy, sh.top.best, tid);
+    write_row<G>(a, t, finish(q), xy, sh.top.best, tid);
     return;
   }
   Gathered& all = *reinterpret_cast<Gathered*>(raw + (sizeof(Shared<G>) + 15) / 16 * 16);
@@ -596,7 +612,7 @@ __global__ void __launch_bounds__(kThreads, 5) scores_kernel(Scores a) {
     __syncthreads();
     rank_keys<G>(sh.top, sh.top.key, ranks * a.k, a.k, tid);
   }
-  write_row(a, t, finish(make_float3(m, sum, log)), xy, sh.top.best, tid);
+  write_row<G>(a, t, finish(make_float3(m, sum, log)), xy, sh.top.best, tid);
 }
 
 // ---- short rows --------------------------------------------------------------------
@@ -624,6 +640,41 @@ __device__ __forceinline__ float group_add(float v) {
 #pragma unroll
   for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
+}
+// Keys of a short row: 32 bits for bf16 logits, whose classes are below 2^16.  0: no alternative.
+template <typename E>
+struct ShortKey {
+  using T = Key;
+  __device__ __forceinline__ static T of(float f, int v) { return f > -INFINITY ? key_of(f, (unsigned)v) : 0; }
+  __device__ __forceinline__ static int at(T q) { return class_of(q); }
+  __device__ __forceinline__ static float value(T q) { return value_of(q); }
+};
+template <>
+struct ShortKey<__nv_bfloat16> {
+  using T = uint32_t;
+  __device__ __forceinline__ static T of(float f, int v) {
+    const uint32_t b = __float_as_uint(f + 0.f);
+    return f > -INFINITY ? ((b ^ ((int32_t)b < 0 ? 0xffffffffu : 0x80000000u)) & 0xffff0000u) | (0xffffu - v) : 0;
+  }
+  __device__ __forceinline__ static int at(T q) { return (int)(0xffffu - (q & 0xffffu)); }
+  __device__ __forceinline__ static float value(T q) {
+    return __uint_as_float((q ^ (q & 0x80000000u ? 0x80000000u : 0xffffffffu)) & 0xffff0000u);
+  }
+};
+// Odd-even merge sort (Batcher) of a power of two of keys, largest first.
+template <typename T, int R>
+__device__ __forceinline__ void sort_down(T (&q)[R]) {
+#pragma unroll
+  for (int p = 1; p < R; p *= 2)
+#pragma unroll
+    for (int d = p; d >= 1; d /= 2)
+#pragma unroll
+      for (int i = 0; i + d < R; ++i)
+        if (i >= d % p && (i - d % p) % (2 * d) < d && i / (2 * p) == (i + d) / (2 * p)) {
+          const T one = q[i], two = q[i + d];
+          q[i] = one > two ? one : two;
+          q[i + d] = one > two ? two : one;
+        }
 }
 template <typename E, int L, int R, int P>
 __global__ void __launch_bounds__(kThreads) short_scores_kernel(Scores a) {
@@ -655,39 +706,35 @@ __global__ void __launch_bounds__(kThreads) short_scores_kernel(Scores a) {
     a.entropy[t] = r.z;
     a.stats[t] = make_float2(r.x, r.y);
   }
-  // one after another: the group's largest, of equal ones the lower class; L of them are written at once
-  int of = -1;
-  float q = -INFINITY;
-  for (int i = 0; i < a.k; ++i) {
-    float best = -INFINITY;
-    int at = INT32_MAX;
+  if (!a.k) return;
+  // A lane's keys, sorted, lie in its column of shared memory; the group's largest head is taken k times, and L of
+  // them are written at once.
+  using Short = typename ShortKey<E>::T;
+  __shared__ Short list[R * kThreads];
+  Short key[R];
 #pragma unroll
-    for (int j = 0; j < R; ++j)
-      if (v[j] > best) {
-        best = v[j];
-        at = short_at<L, P>(l, j);
-      }
+  for (int j = 0; j < R; ++j) key[j] = ShortKey<E>::of(v[j], short_at<L, P>(l, j));
+  sort_down(key);
+#pragma unroll
+  for (int j = 1; j < R; ++j) list[j * kThreads + threadIdx.x] = key[j];
+  Short head = key[0], kept = 0;
+  int next = 1;
+  for (int i = 0; i < a.k; ++i) {
+    Short best = head;
 #pragma unroll
     for (int o = L / 2; o > 0; o >>= 1) {
-      const float f = __shfl_xor_sync(0xffffffffu, best, o);
-      const int e = __shfl_xor_sync(0xffffffffu, at, o);
-      if (f > best || (f == best && e < at)) {
-        best = f;
-        at = e;
-      }
+      const Short other = __shfl_xor_sync(0xffffffffu, best, o);
+      best = other > best ? other : best;
     }
-    const bool any = best > -INFINITY;
-#pragma unroll
-    for (int j = 0; j < R; ++j)
-      if (any && short_at<L, P>(l, j) == at) v[j] = -INFINITY;
-    if (l == i % L) {
-      of = any ? at : -1;
-      q = any ? (best - r.x) * a.inv_tau - r.y : -INFINITY;
+    if (best != 0 && head == best) {
+      head = next < R ? list[next * kThreads + threadIdx.x] : 0;
+      ++next;
     }
+    if (l == i % L) kept = best;
     const int first = i / L * L;
     if ((i % L == L - 1 || i == a.k - 1) && t < a.T && first + l <= i) {
-      a.top[t * a.k + first + l] = of;
-      a.top_logp[t * a.k + first + l] = q;
+      a.top[t * a.k + first + l] = kept ? ShortKey<E>::at(kept) : -1;
+      a.top_logp[t * a.k + first + l] = kept ? (ShortKey<E>::value(kept) - r.x) * a.inv_tau - r.y : -INFINITY;
     }
   }
 }
@@ -885,7 +932,7 @@ struct Shape {
 Shape shape_of(const pgc_logits* z, int k) {
   const int64_t bytes = z->classes * (z->dtype == PGC_BF16 ? 2 : 4), sms = sm_count();
   const int64_t many = k ? kWarpManyTopBytes : kWarpManyRowsBytes;
-  Shape s{k <= kWarpTop && (bytes <= kWarpRowBytes || (bytes <= many && z->rows >= 32 * sms)), 1, 0};
+  Shape s{bytes <= kWarpRowBytes || (bytes <= many && z->rows >= 32 * sms), 1, 0};
   if (s.warp) {
     s.grid = (unsigned)((z->rows + kWarps - 1) / kWarps);
     return s;
@@ -944,7 +991,7 @@ struct ShortGrad {
 
 template <typename E>
 cudaError_t launch_scores(const Scores& a, const Shape& s, cudaStream_t st) {
-  const auto kernel = s.warp ? scores_kernel<E, 32> : scores_kernel<E, kThreads>;
+  const auto kernel = !s.warp ? scores_kernel<E, kThreads, false> : a.k > 32 ? scores_kernel<E, 32, true> : scores_kernel<E, 32, false>;
   size_t smem = s.warp ? sizeof(Shared<32>) * kWarps : sizeof(Shared<kThreads>);
   if (s.ranks > 1) smem = (smem + 15) / 16 * 16 + sizeof(Gathered);
   cudaLaunchAttribute attr;
