@@ -564,7 +564,7 @@ int pgc_token_scores_grad(const pgc_logits *z, const float *stats, const float *
  *    have a row differ from one another.
  *  - Rows of the experts' order that no slot has are left as they were.
  *  - Sums run over j in order, in 32 bits; a bf16 result is rounded once.
- *  - rows, tokens < 2^31 and tokens k < 2^31, 1 <= d < 2^31, d <= pitch <= 2^31; k <= 64 and experts <= 1024,
+ *  - rows, tokens < 2^31 and tokens k < 2^31, 1 <= d <= 2^30, d <= pitch <= 2^31; k <= 64 and experts <= 1024,
  *    PGC_ENOTSUP above.  No output overlaps an input, but where it says so.
  */
 
@@ -643,7 +643,7 @@ typedef struct pgc_adamw_tensor {
 typedef struct pgc_adamw {
   double lr, beta1, beta2, eps, weight_decay;
   int64_t step;               /* 1 for the first one                               */
-  const int64_t *step_at;     /* device: in place of step; or NULL                 */
+  const int64_t *step_at;     /* device, at least 1: in place of step; or NULL     */
   const float *lr_at;         /* device: in place of lr; or NULL                   */
   const float *grad_scale;    /* device: factor of the gradients; or NULL for 1    */
   uint32_t seed;

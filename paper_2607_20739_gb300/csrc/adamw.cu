@@ -139,13 +139,14 @@ struct Share {
     }
     tensor = lo;
   }
-  // The next part: its tensor, the first of its blocks there and how many; 2^32 elements of a tensor are never crossed.
+  // The next part: its tensor, the first of its blocks there and how many; 2^31 elements of a tensor are never
+  // crossed, so that an index within a part is 32 bits, and the upper half of an element's the same in all of it.
   __device__ __forceinline__ bool next(const Table& a, int* of, uint32_t* block, uint32_t* count) {
     if (at >= end) return false;
     while (at >= a.first[tensor + 1]) ++tensor;
     *of = tensor;
     *block = at - a.first[tensor];
-    constexpr uint32_t kSide = 1u << 24;
+    constexpr uint32_t kSide = 1u << 23;
     *count = min(min(end, a.first[tensor + 1]) - at, kSide - *block % kSide);
     at += *count;
     return true;

@@ -462,6 +462,7 @@ __global__ void __launch_bounds__(kThreads, Q == 2 ? 4 : 3) join_grad_kernel(Mov
 // ---- host --------------------------------------------------------------------
 
 constexpr int64_t kFarPitch = int64_t(1) << 31;
+constexpr int64_t kMostWidth = 1 << 30;         // an index of elements that steps beyond a row stays an int
 constexpr size_t kPlainSmem = 36 * 1024;         // beside 8 KB of fixed size, without asking
 
 int check_sizes(int64_t tokens, int32_t k) {
@@ -474,7 +475,7 @@ bool bad_rows(const void* p, int64_t count, int64_t d, int64_t ld, uintptr_t siz
 }
 int check_move(int32_t dtype, int64_t tokens, int32_t k, int64_t d, int64_t rows, const int32_t* place) {
   if (dtype != PGC_F32 && dtype != PGC_BF16) return PGC_EINVAL;
-  if (tokens < 0 || k < 1 || tokens > INT32_MAX / k || d < 1 || d > INT32_MAX || rows < 0 || rows > INT32_MAX) return PGC_EINVAL;
+  if (tokens < 0 || k < 1 || tokens > INT32_MAX / k || d < 1 || d > kMostWidth || rows < 0 || rows > INT32_MAX) return PGC_EINVAL;
   return (tokens && !place) || (uintptr_t)place % 4 ? PGC_EINVAL : PGC_OK;
 }
 

@@ -83,6 +83,8 @@ class AdamW:
             raise ValueError("the number of steps must not be negative")
         self._device_step = torch.full((), t, dtype=torch.int64, device=self.device) if device_step and self.params else None
         self._t = t
+        # inference tensors have no version
+        self._versioned = [t for t in self.params + (self.copies or []) if not t.is_inference()]
         self._shapes = [p.shape for p in self.params]
         self._devices = [p.get_device() for p in self.params]
         self._table = (B.AdamWTensor * len(self.params))()
@@ -181,4 +183,4 @@ class AdamW:
             kept = [t for group in kept for t in group]
         _on(device, stream, kept, call)
         self._t += 1
-        torch.autograd.graph.increment_version(self.params if self.copies is None else self.params + self.copies)
+        torch.autograd.graph.increment_version(self._versioned)

@@ -356,3 +356,69 @@ def test_small_gradients_and_eps(cuda, optim, bits, eps):
     got = on_host(p)
     sure = np.isfinite(low)
     assert sure.sum() > n / 3 and (np.abs(got - (0.5 - step)) <= tol * 1.01)[sure].all()
+
+
+def test_inference_tensors(cuda, optim):
+    """Parameters without a version counter; a captured step's tensors as well as others' on the default stream."""
+    torch = cuda
+    with torch.inference_mode():
+        p, g = torch.ones(300, device="cuda"), torch.ones(300, device="cuda")
+    opt = optim.AdamW([p], lr=0.5, weight_decay=0.0)
+    opt.step([g])
+    assert ((p - 0.5).abs() <= 40 * U).all()
+
+
+def test_a_changed_parameter_is_noticed(cuda, optim):
+    """A backward pass over a graph that kept a parameter's older value is refused."""
+    torch = cuda
+    p = torch.ones(10, device="cuda", requires_grad=True)
+    y = (p * p).sum()
+    optim.AdamW([p]).step([torch.ones(10, device="cuda")])
+    with pytest.raises(RuntimeError, match="modified"):
+        y.backward()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("ptype,gtype", [("float32", "bfloat16"), ("bfloat16", "bfloat16")])
+def test_large_tensors(cuda, optim, bits, ptype, gtype):
+    """Tens of millions of elements in tensors of which one starts anywhere: here and there against the oracle, and all
+    of them against the same step over parts."""
+    torch = cuda
+    ptype, gtype = getattr(torch, ptype), getattr(torch, gtype)
+    sizes = [5_000_003, 1, 777, 9_000_000, 4_000_001, 300]
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    params = [(torch.randn(n + 1, generator=gen, device="cuda") * 0.05).to(ptype)[i == 4:][:n] for i, n in enumerate(sizes)]
+    grads = [(torch.randn(n + 1, generator=gen, device="cuda") * 1e-3).to(gtype)[i == 4:][:n] for i, n in enumerate(sizes)]
+    old = [p.clone() for p in params]
+    kw = dict(lr=1e-2, betas=(0.9, 0.95), weight_decay=0.1, bits=bits, seed=11)
+    opt = optim.AdamW(params, **kw)
+    opt.step(grads)
+    opt.step(grads)
+    r = np.random.default_rng(0)
+    for i, n in enumerate(sizes):
+        blocks = -(-n // 256)
+        for b in sorted({0, blocks - 1, *r.integers(0, blocks, 12).tolist()}):
+            s, e = b * 256, min(n, b * 256 + 256)
+            g, p = on_host(grads[i][s:e]).astype(np.float32), on_host(old[i][s:e])
+            m = v = np.zeros(e - s)
+            mc = vc = np.zeros(e - s, np.uint8)
+            ms = vs = np.zeros(1, np.float32)
+            for t in (1, 2):
+                if bits == 8:
+                    m, v = O.decode_m(mc) * ms[0], O.decode_v(vc) * vs[0]
+                    q, mc, vc, ms, vs = O.adamw8(p, g, mc, vc, ms, vs, t, i, 11, (0.9, 0.95), index=s, lr=1e-2, decay=0.1)
+                    _, m1, _, step, em = expected(p, g.astype(np.float64), m, v, t, 1e-2, (0.9, 0.95), 1e-8, 0.1)
+                else:
+                    q, m1, v1, step, em = expected(p, g.astype(np.float64), m, v, t, 1e-2, (0.9, 0.95), 1e-8, 0.1)
+                    m, v = m1.astype(np.float32).astype(np.float64), v1.astype(np.float32).astype(np.float64)
+                if t == 1:                              # the parameter that the second step starts from is a rounded one
+                    p = q.astype(np.float32).astype(np.float64) if ptype == torch.float32 else \
+                        torch.from_numpy(q).to(torch.float32).to(ptype).double().numpy()
+            if bits == 8:
+                assert (opt.m[i][s:e].view(torch.uint8).cpu().numpy() == mc).all()
+                assert (opt.v[i][s:e].cpu().numpy() == vc).all()
+            # the first step's error again in the second's, and its rounding that may have gone the other way
+            h = torch.finfo(ptype).eps / 2
+            err = np.abs(on_host(params[i][s:e]) - q)
+            tol = 2 * (np.abs(step) * 40 * U + 8 * U * np.abs(p)) + 3 * h * np.abs(q)
+            assert (err <= tol).all(), (i, b, (err / tol).max())

@@ -273,3 +273,35 @@ def test_route_of_sorted_and_blocked_choices(cuda, experts, T, k, E):
     c = (np.arange(T * k) * E // (T * k)).astype(np.int32).reshape(T, k)
     for choice in (c, c[::-1].copy(), np.where(c % 3 == 1, -5, c).astype(np.int32)):
         check_routes(experts.route(torch.from_numpy(choice).cuda(), E), choice, E)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("k,d,pad,shift", [(1, 8, 0, 0), (2, 30, 0, 0), (3, 33, 0, 0), (3, 33, 3, 1), (5, 100, 4, 2), (9, 257, 0, 0), (8, 260, 0, 4), (4, 513, 1, 0)])
+def test_moves_of_many_tokens(cuda, experts, dtype, k, d, pad, shift):
+    """A token per warp."""
+    torch = cuda
+    dtype, T = getattr(torch, dtype), 5003
+    h = torch.finfo(dtype).eps / 2
+    N = T * k - 5
+    place = place_of(torch, T, k, N, seed=d)
+    r = routes_of(torch, experts, place)
+    x, dy, e = (rows(torch, dtype, n, d, pad, shift, seed) for seed, n in ((1, T), (2, T), (3, N)))
+    w = torch.from_numpy(np.random.default_rng(d).standard_normal((T, k)).astype(np.float32)).cuda()
+    on = torch.from_numpy((place >= 0) & (place < N)).cuda()
+    at = torch.from_numpy(np.where((place >= 0) & (place < N), place, 0)).cuda().long()
+    token = torch.arange(T, device="cuda")[:, None].expand(T, k)
+    out = torch.full((N, d), 7.0, dtype=dtype, device="cuda")
+    experts.spread(x, r, out=out)
+    want = torch.full((N, d), 7.0, dtype=dtype, device="cuda")
+    want[at[on]] = x[token[on]]
+    assert torch.equal(out, want)
+    terms = e.double()[at] * w.double()[:, :, None] * on[:, :, None]
+    y, size = terms.sum(1), terms.abs().sum(1)
+    assert ((experts.join(e, r, w).double() - y).abs() <= U * (k + 1) * size * (1 + h) + h * y.abs()).all()
+    drows, dweight = experts.join_grad(dy, e, r, w, out=torch.full((N, d), 7.0, dtype=dtype, device="cuda"))
+    full = torch.full((N, d), 7.0, dtype=torch.float64, device="cuda")
+    full[at[on]] = (w.double()[:, :, None] * dy.double()[:, None, :])[on]
+    assert ((drows.double() - full).abs() <= (h + (2 * U if h > U else 0)) * full.abs()).all()
+    terms = e.double()[at] * dy.double()[:, None, :] * on[:, :, None]
+    chain = min(d, d / 32 + 64) + 1
+    assert ((dweight.double() - terms.sum(2)).abs() <= U * chain * terms.abs().sum(2)).all()

@@ -334,3 +334,80 @@ def test_classes_beyond_32_bits_of_bytes(cuda, losses):
     check_gradient(torch, g, small, y, a, b, 1.0)
     del store, x, g
     torch.cuda.empty_cache()
+
+
+def some_rows(torch, r, x, y, rows):
+    at = torch.tensor(rows, device="cuda")
+    part = {k: None if v is None else v[at] for k, v in r.items()}
+    return part, x[at], None if y is None else y[at]
+
+
+@pytest.mark.parametrize("dtype,V", [("bfloat16", 2500), ("bfloat16", 9000), ("bfloat16", 33001), ("float32", 1200), ("float32", 9001), ("float32", 17000)])
+@pytest.mark.parametrize("k", [0, 1, 20, 32, 33, 64])
+def test_many_longer_rows(cuda, losses, dtype, V, k):
+    """So many rows that a warp takes one of up to 72 KB: against the oracle here and there, special rows among them, and
+    against the calls on fewer rows everywhere."""
+    torch = cuda
+    dtype, T = getattr(torch, dtype), 5200
+    g = torch.Generator(device="cuda").manual_seed(V + k)
+    x = torch.empty(T, V, dtype=dtype, device="cuda")
+    for t in range(0, T, 400):
+        x[t:t + 400] = torch.randn((400, V), generator=g, device="cuda") * 2
+    y = torch.randint(V, (T,), generator=g, device="cuda").to(torch.int32)
+    y[5::7] = -1
+    x[10] = 0.0                                              # all equal
+    x[11, 3:] = float("-inf")                                # fewer than most k left
+    x[12] = float(torch.finfo(dtype).min)                    # masked by a number
+    x[12, V // 2:V // 2 + 9] = 1.5
+    x[13] = torch.linspace(-3, 9, V, device="cuda").to(dtype)     # rising
+    x[14, ::2] = 5.0                                         # many of the largest
+    y[10:15] = 4
+    y[11] = 2
+    r = losses.token_scores(x, y, k)
+    part, xs, ys = some_rows(torch, r, x, y, list(range(0, 40)) + [2600, T - 2, T - 1])
+    check_scores(torch, part, xs, ys, k, 1.0)
+    for t in range(0, T, 1300):
+        few = losses.token_scores(x[t:t + 1300], y[t:t + 1300], k)
+        assert torch.equal(few["top"], r["top"][t:t + 1300])
+        # both within the bound of logp and entropy, here 1e-4 of a few units at most
+        for name in ("logp", "entropy", "top_logp"):
+            a, b = few[name], r[name][t:t + 1300]
+            assert ((a - b).abs() <= 1e-4 * (1 + b.abs()) * (1 + V ** 0.5 * 1e-2))[torch.isfinite(b)].all() and \
+                torch.equal(torch.isfinite(a), torch.isfinite(b))
+    if k in (0, 20):
+        a, b = (torch.randn(T, generator=g, device="cuda") for _ in range(2))
+        d = losses.token_scores_grad(x, y, r["stats"], r["entropy"], a, b)
+        rows = list(range(0, 25)) + [T - 2, T - 1]
+        at = torch.tensor(rows, device="cuda")
+        check_gradient(torch, d[at], x[at], y[at], on_host(a[at]), on_host(b[at]), 1.0)
+        assert (d[y < 0] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("V", [3, 17, 64, 100, 129, 200, 256, 301, 511, 512])
+@pytest.mark.parametrize("k", [1, 9, 64])
+def test_short_rows(cuda, losses, dtype, V, k):
+    """Several rows to a warp: the last warp is not full; special rows among them."""
+    torch = cuda
+    dtype = getattr(torch, dtype)
+    _, x, y = make(torch, dtype, 203, V, masked=range(2, 203, 5))
+    x[0] = 1.0
+    x[1, V // 2:] = float("-inf")
+    y[1] = 0
+    x[3] = float(torch.finfo(dtype).min)
+    x[3, V - 1] = 2.0
+    y[3] = V - 1
+    x[4, ::2] = 0.0
+    x[4, 1::2] = -0.0
+    y[4] = V - 1
+    r = losses.token_scores(x, y, k, 0.9)
+    check_scores(torch, r, x, y, k, 0.9)
+    a, b, da, db = derivatives(torch, 203)
+    check_gradient(torch, losses.token_scores_grad(x, y, r["stats"], r["entropy"], da, db, 0.9), x, y, a, b, 0.9)
+    x[5, V // 2] = float("nan")
+    x[6, V // 2] = float("inf")
+    y[5:7] = 0
+    r = losses.token_scores(x, y, k)
+    assert torch.isnan(r["logp"][5:7]).all() and torch.isnan(r["entropy"][5:7]).all()
+    assert r["top"][6, 0] == V // 2 and V // 2 not in r["top"][5].tolist()
+    assert torch.isfinite(r["logp"][7:]).all()

@@ -102,7 +102,7 @@ def join_grad(B, dtype=1, tokens=4, k=2, d=16, dy=P, dy_ld=16, x=P, ld=16, rows=
     return B.lib.pgc_join_grad(dtype, tokens, k, d, dy, dy_ld, x, ld, rows, place, weight, out, out_ld, dweight, None)
 
 
-@pytest.mark.parametrize("kw", [dict(dtype=2), dict(tokens=-1), dict(k=0), dict(tokens=1 << 30, k=2), dict(d=0), dict(d=1 << 31),
+@pytest.mark.parametrize("kw", [dict(dtype=2), dict(tokens=-1), dict(k=0), dict(tokens=1 << 30, k=2), dict(d=0), dict(d=1 << 31), dict(d=(1 << 30) + 1, ld=1 << 31, out_ld=1 << 31),
                                 dict(ld=15), dict(out_ld=15), dict(ld=(1 << 31) + 1), dict(rows=-1), dict(rows=1 << 31), dict(x=None),
                                 dict(out=None), dict(place=None), dict(place=P + 2), dict(x=P + 1), dict(out=P + 1),
                                 dict(dtype=0, x=P + 2), dict(dtype=0, out=P + 2)])
