@@ -249,8 +249,9 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
 // Codes of four elements, and their values before the scale.  What follows counts instructions: at
 // 10 bytes an element (bf16 parameters and gradients) an SM has 55 issue slots for it while its share of memory moves, and
 // its unit of compares, shifts and logic half as many.  So shifts to the left are products, choices maxima, and a
-// second moment's values a table.  60 instructions an element are left (82 as first written: 236 us for 72 M, 150 now, 5.1 TB/s; with
-// fp32 parameters memory is the bound, 6.6 TB/s).
+// second moment's values a table; what is rare (a value below the lowest code, a block without a scale) is put right
+// behind a branch.  About 58 instructions an element are left (82 as first written), and they are the bound: 75 M in 150 us, 5.1 TB/s.
+// With fp32 parameters memory is, 6.6 TB/s.
 __device__ __forceinline__ Four decode_m(uint32_t codes) {
   uint32_t lo, hi;
   asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
@@ -280,11 +281,10 @@ __device__ __forceinline__ uint32_t encode_m(float y, uint32_t chance) {
   const int w = __viaddmax_s32(__float_as_int(__fadd_rz(y, 0x1p-6f)), -(1 << 23), __float_as_int(y));
   return (uint32_t)w * 16u + chance;                        // - (120 << 23) 16 is 0x40 in the upper byte
 }
-// Sixteen codes an octave from 2^-3 on, eight below: again the larger place.  At least 1, but 0 for 0.
-__device__ __forceinline__ uint32_t encode_v(float y, uint32_t chance) {
-  const int b = max(__float_as_int(y), 866 << 20);
-  const int w = __viaddmax_s32(b, -(1857 << 20), -(865 << 20)) + b;
-  return ((uint32_t)w * 16u + chance) * min(__float_as_uint(y), 1u);
+// Sixteen codes an octave from 2^-3 on, eight below: again the larger place.  y as bits, those of code 1 at least.
+constexpr int kLowestCode = 866 << 20;
+__device__ __forceinline__ uint32_t encode_v(int y, uint32_t chance) {
+  return (uint32_t)(__viaddmax_s32(y, -(1857 << 20), -(865 << 20)) + y) * 16u + chance;
 }
 // The upper bytes of four words.
 __device__ __forceinline__ uint32_t bytes4(const uint32_t (&c)[4]) {
@@ -370,22 +370,23 @@ __device__ __forceinline__ void step8(Pair (&p)[kPairs], const Pair (&g)[kPairs]
       vt = __vimax3_u32(vt, __float_as_uint(lo), __float_as_uint(hi));
     }
   }
-  // Scales as bits.  A magnitude's exponent is 16 to 254, or its block's codes are zeros and the scale
-  // is 0 or NaN.  An m' that is NaN has a v' that is, or an old scale that was.
+  // Scales as bits.  A block's largest exponents are 16 to 254, or its codes are zeros and the scale is
+  // 0 or NaN.  An m' that is NaN has a v' that is, or an old scale that was.
   const uint32_t m_top = __reduce_max_sync(0xffffffffu, __float_as_uint(mt)) & 0x7f800000u;
-  const uint32_t v_bits = __reduce_max_sync(0xffffffffu, vt), v_top = v_bits & 0x7f800000u;
+  const uint32_t v_top = __reduce_max_sync(0xffffffffu, vt) & 0x7f800000u;
   constexpr uint32_t kLow = 16u << 23, kRange = 239u << 23;
-  const bool m_ok = m_top - kLow < kRange && !isnan(ms), v_ok = v_top - kLow < kRange;
-  const bool lost = v_top == 0x7f800000u;
+  const bool usual = m_top - kLow < kRange && v_top - kLow < kRange && !isnan(ms);
   const float mo = __uint_as_float((261u << 23) - m_top), vo = __uint_as_float((258u << 23) - v_top);
-  ms = m_ok && !lost ? __uint_as_float(m_top - (7u << 23)) : m_top == 0x7f800000u || isnan(ms) || lost ? NAN : 0.f;
-  vs = v_ok ? __uint_as_float(v_top - (4u << 23)) : lost ? NAN : 0.f;
+  const float old_ms = ms;
+  ms = __uint_as_float(m_top - (7u << 23));
+  vs = __uint_as_float(v_top - (4u << 23));
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     // the first step of mix is that of all four but for the last two bits of an index
     uint32_t first = (index + 128 * h) ^ key;
     first ^= first >> 16;
-    uint32_t cm[4], cv[4];
+    uint32_t cm[4], cv[4], of_v[4];
+    int y[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       uint32_t x = (first ^ j) * kOdd1;
@@ -397,14 +398,28 @@ __device__ __forceinline__ void step8(Pair (&p)[kPairs], const Pair (&g)[kPairs]
       split(v[2 * h + j / 2], lo, hi);
       const float vj = j % 2 ? hi : lo;
       cm[j] = encode_m(__fmul_rn(fabsf(mj), mo), chance.m) | (__float_as_uint(mj) & 0x80000000u);
-      cv[j] = encode_v(__fmul_rn(vj, vo), chance.v);
+      y[j] = __float_as_int(__fmul_rn(vj, vo));
+      of_v[j] = chance.v;
+      cv[j] = encode_v(y[j], chance.v);
+    }
+    // some below the lowest code: that one, but 0 for 0
+    if (min(__vimin3_s32(y[0], y[1], y[2]), y[3]) < kLowestCode) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) cv[j] = y[j] ? encode_v(max(y[j], kLowestCode), of_v[j]) : 0;
     }
     mc[h] = bytes4(cm);
     vc[h] = bytes4(cv);
   }
-  if (!(m_ok && v_ok)) {
-    if (!m_ok || lost) mc[0] = mc[1] = 0;
-    if (!v_ok) vc[0] = vc[1] = 0;
+  if (!usual) {
+    const bool v_lost = v_top == 0x7f800000u, m_lost = m_top == 0x7f800000u || v_lost || isnan(old_ms);
+    if (m_lost || m_top < kLow) {
+      ms = m_lost ? NAN : 0.f;
+      mc[0] = mc[1] = 0;
+    }
+    if (v_lost || v_top < kLow) {
+      vs = v_lost ? NAN : 0.f;
+      vc[0] = vc[1] = 0;
+    }
   }
 }
 
