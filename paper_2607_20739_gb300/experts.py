@@ -13,7 +13,8 @@ consecutive rows, and what the experts made of them is added at the tokens:
 
 Thin layer over the calls of include/pgc.h, as ``losses``; nothing here is
 recorded by autograd.  Rows are float32 or bfloat16, their elements contiguous (any
-row pitch); ``out`` is a tensor for the result; ``stream`` as in ``losses``.
+row pitch); ``out`` is a tensor for the result that shares no element with the arguments; ``stream`` as
+in ``losses``.
 """
 
 from __future__ import annotations
@@ -74,12 +75,39 @@ def _rows(name, t, routes, count=None, like=None):
     return rows, d, ld
 
 
-def _result(out, rows, routes, like):
-    """The tensor for `rows` rows and its pitch; made anew unless given."""
+def _share(a, b):
+    """Whether two matrices of rows have an element in common."""
+    (rows_a, d, ld_a), (rows_b, _, ld_b), size = _matrix("out", a), _matrix("rows", b), a.element_size()
+    if not rows_a or not rows_b:
+        return False
+    start_a, start_b = a.data_ptr(), b.data_ptr()
+    if start_a + ((rows_a - 1) * ld_a + d) * size <= start_b or start_b + ((rows_b - 1) * ld_b + d) * size <= start_a:
+        return False
+    if rows_a < 2 or rows_b < 2:
+        pitch = max(a.stride(0), b.stride(0))
+    elif ld_a == ld_b:
+        pitch = ld_a
+    else:
+        return True
+    # columns beside one another in rows of a common pitch
+    apart = (start_b - start_a) % (pitch * size)
+    return not d * size <= apart <= (pitch - d) * size
+
+
+def _same(a, b):
+    """Whether the rows of two matrices are the same memory."""
+    return a is not None and a.data_ptr() == b.data_ptr() and a.stride() == b.stride()
+
+
+def _result(out, rows, routes, like, *inputs):
+    """The tensor for `rows` rows and its pitch; made anew unless given, then apart from the inputs."""
     if out is None:
         d = like.shape[1]
         return torch.empty((rows, d), dtype=like.dtype, device=like.device), d
-    return out, _rows("out", out, routes, rows, like)[2]
+    ld = _rows("out", out, routes, rows, like)[2]
+    if any(_share(out, t) for t in inputs):
+        raise ValueError("out must not share memory with the other rows")
+    return out, ld
 
 
 def spread(x, routes, *, out=None, stream=None):
@@ -89,7 +117,7 @@ def spread(x, routes, *, out=None, stream=None):
     rows = routes.tokens * routes.k if out is None else _rows("out", out, routes, None, x)[0]
 
     def call(st):
-        result, ldo = _result(out, rows, routes, x)
+        result, ldo = _result(out, rows, routes, x, x)
         B._check(B.lib.pgc_spread(_TYPES[x.dtype], routes.tokens, routes.k, d, x.data_ptr(), ld, routes.place.data_ptr(),
                                   rows, result.data_ptr(), ldo, st), "pgc_spread")
         return result
@@ -103,7 +131,7 @@ def join(rows, routes, weight=None, *, out=None, stream=None):
         _vector("weight", weight, torch.float32, (routes.tokens, routes.k), rows.device)
 
     def call(st):
-        result, ldo = _result(out, routes.tokens, routes, rows)
+        result, ldo = _result(out, routes.tokens, routes, rows, rows)
         B._check(B.lib.pgc_join(_TYPES[rows.dtype], routes.tokens, routes.k, d, rows.data_ptr(), ld, n,
                                 routes.place.data_ptr(), _address(weight), result.data_ptr(), ldo, st), "pgc_join")
         return result
@@ -123,7 +151,7 @@ def join_grad(dy, rows, routes, weight, *, out=None, stream=None):
     _vector("weight", weight, torch.float32, (routes.tokens, routes.k), rows.device)
 
     def call(st):
-        drows, ldo = _result(out, n, routes, rows)
+        drows, ldo = _result(out, n, routes, rows, dy, *(() if _same(out, rows) else (rows,)))
         dweight = torch.empty((routes.tokens, routes.k), dtype=torch.float32, device=rows.device)
         B._check(B.lib.pgc_join_grad(_TYPES[rows.dtype], routes.tokens, routes.k, d, dy.data_ptr(), ldy, rows.data_ptr(), ld,
                                      n, routes.place.data_ptr(), weight.data_ptr(), drows.data_ptr(), ldo,

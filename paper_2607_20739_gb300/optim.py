@@ -56,7 +56,8 @@ class AdamW:
     state         moments and step to go on from, as ``state()`` returns them (the tensors
                   themselves are used); default: zeros
     device_step   the number of steps is kept on the device, so that a captured step
-                  counts itself when it is replayed
+                  counts itself when it is replayed; without it a step under capture is refused.  Rates that
+                  are floats are those of the capture in every replay
     """
 
     def __init__(self, params, *, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, bits=32, copies=None, seed=0,
@@ -64,6 +65,23 @@ class AdamW:
         self.params = list(params)
         if bits not in (8, 32):
             raise ValueError("bits must be 8 or 32")
+        self._check_params()
+        self.device = self.params[0].device if self.params else None
+        self.lr, self.betas, self.eps, self.weight_decay, self.bits, self.seed = lr, betas, eps, weight_decay, bits, seed
+        self.copies = None if copies is None else _list("copies", copies, self.params, torch.bfloat16)
+        self._moments(state)
+        t = 0 if state is None else int(state["t"])
+        if t < 0:
+            raise ValueError("the number of steps must not be negative")
+        self._device_step = torch.full((), t, dtype=torch.int64, device=self.device) if device_step and self.params else None
+        self._t = t
+        self._table = (B.AdamWTensor * len(self.params))()
+        # the column of the gradients' addresses
+        self._grads = np.frombuffer(self._table, dtype=np.int64).reshape(-1, C.sizeof(B.AdamWTensor) // 8)[
+            :, B.AdamWTensor.grad.offset // 8] if self.params else None
+        self._fill()
+
+    def _check_params(self):
         for i, p in enumerate(self.params):
             if not isinstance(p, torch.Tensor):
                 raise TypeError(f"params[{i}] must be a torch tensor")
@@ -72,41 +90,43 @@ class AdamW:
             if p.dtype not in _TYPES or p.dtype != self.params[0].dtype:
                 raise ValueError("parameters must be float32 or bfloat16, all of one type")
             _vector(f"params[{i}]", p, p.dtype, tuple(p.shape), self.params[0].device)
-        self.device = self.params[0].device if self.params else None
-        self.lr, self.betas, self.eps, self.weight_decay, self.bits, self.seed = lr, betas, eps, weight_decay, bits, seed
-        self.copies = None if copies is None else _list("copies", copies, self.params, torch.bfloat16)
-        self._moments(state)
-        kept = [self.m, self.v, self.m_scale or [], self.v_scale or [], self.copies or []]
-        _refuse_overlaps(self.params + [t for group in kept for t in group])
-        t = 0 if state is None else int(state["t"])
-        if t < 0:
-            raise ValueError("the number of steps must not be negative")
-        self._device_step = torch.full((), t, dtype=torch.int64, device=self.device) if device_step and self.params else None
-        self._t = t
-        # inference tensors have no version
-        self._versioned = [t for t in self.params + (self.copies or []) if not t.is_inference()]
-        self._shapes = [p.shape for p in self.params]
-        self._devices = [p.get_device() for p in self.params]
-        self._table = (B.AdamWTensor * len(self.params))()
-        # the column of the gradients' addresses
-        self._grads = np.frombuffer(self._table, dtype=np.int64).reshape(-1, C.sizeof(B.AdamWTensor) // 8)[
-            :, B.AdamWTensor.grad.offset // 8] if self.params else None
+
+    def _fill(self):
+        """The table of all tensors but the gradients, from where they lie now."""
+        copies = self.copies or []
+        moments = [t for group in (self.m, self.v, self.m_scale or [], self.v_scale or []) for t in group]
+        _refuse_overlaps(self.params + copies + moments)
         for i, p in enumerate(self.params):
             e = self._table[i]
             e.param, e.m, e.v, e.n = p.data_ptr(), self.m[i].data_ptr(), self.v[i].data_ptr(), p.numel()
-            e.copy = None if self.copies is None else self.copies[i].data_ptr()
-            if bits == 8:
+            e.copy = copies[i].data_ptr() if copies else None
+            if self.bits == 8:
                 e.m_scale, e.v_scale = self.m_scale[i].data_ptr(), self.v_scale[i].data_ptr()
+        self._shapes = [p.shape for p in self.params]
+        self._devices = [p.get_device() for p in self.params]
+        given = self.params + copies
+        self._at = list(map(_address_of, given))
+        # inference tensors have no version
+        self._versioned = [t for t in given if not t.is_inference()]
+
+    def _moved(self):
+        """Parameters or copies whose data has been exchanged (``p.data = ...``): looked at anew."""
+        self._check_params()
+        for i, (p, shape) in enumerate(zip(self.params, self._shapes)):
+            _vector(f"params[{i}]", p, p.dtype, shape, self.device)
+        if self.copies is not None:
+            self.copies = _list("copies", self.copies, self.params, torch.bfloat16)
+        self._fill()
 
     def _moments(self, state):
         blocks = lambda p: (-(-p.numel() // BLOCK),)  # noqa: E731
         m_type, v_type = (torch.float32, torch.float32) if self.bits == 32 else (torch.float8_e4m3fn, torch.uint8)
         if state is None:
-            self.m = [torch.zeros(p.shape, dtype=m_type, device=p.device) for p in self.params]
-            self.v = [torch.zeros(p.shape, dtype=v_type, device=p.device) for p in self.params]
+            self.m = tuple(torch.zeros(p.shape, dtype=m_type, device=p.device) for p in self.params)
+            self.v = tuple(torch.zeros(p.shape, dtype=v_type, device=p.device) for p in self.params)
         else:
-            self.m = _list("m", state["m"], self.params, m_type)
-            self.v = _list("v", state["v"], self.params, v_type)
+            self.m = tuple(_list("m", state["m"], self.params, m_type))
+            self.v = tuple(_list("v", state["v"], self.params, v_type))
         self.m_scale = self.v_scale = None
         if self.bits == 8 and state is None:
             self.m_scale, self.v_scale = ([torch.zeros(blocks(p), dtype=torch.float32, device=p.device)
@@ -122,14 +142,14 @@ class AdamW:
 
     def state(self):
         """What ``state`` takes: the step and the moments (the tensors themselves)."""
-        s = {"t": self.t, "m": self.m, "v": self.v}
+        s = {"t": self.t, "m": list(self.m), "v": list(self.v)}
         if self.bits == 8:
-            s["m_scale"], s["v_scale"] = self.m_scale, self.v_scale
+            s["m_scale"], s["v_scale"] = list(self.m_scale), list(self.v_scale)
         return s
 
     def _addresses(self, grads):
         """The gradients' type and addresses, 0 for None; refuses what does not go with the parameters."""
-        # A step of few elements lasts as long as this: five passes of C over the list (0.25 us a tensor), and the
+        # A step of few elements lasts as long as this: five passes of C over the list (0.28 us a tensor), and the
         # loop that finds what is wrong only where something is.
         try:
             kinds = set(map(_dtype_of, grads))
@@ -167,11 +187,15 @@ class AdamW:
                 raise ValueError("grad_scale must have one element")
         if not self.params:
             return
+        if list(map(_address_of, self.params + (self.copies or []))) != self._at:
+            self._moved()
         self._grads[:] = addresses
 
         def call(st):
             if self._device_step is not None:
                 self._device_step.add_(1)
+            elif torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("a step that is captured needs device_step: replays would all be the same step")
             a = B.AdamW(0.0 if lr_at is not None else self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay,
                         self._t + 1, _address(self._device_step), _address(lr_at), _address(grad_scale),
                         self.seed & 0xffffffff, _TYPES[self.params[0].dtype], _TYPES[dtype], self.bits)

@@ -306,6 +306,50 @@ def test_refusals(cuda, optim):
     assert opt.t == 0 and (p == 0).all()
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_exchanged_parameters(cuda, optim, bits):
+    """Parameters and copies whose data is another tensor's since the last step."""
+    torch = cuda
+    r, params, grads = make(torch, [5, 700], torch.float32, torch.float32)
+    other = [p.clone() for p in params]
+    halves, wanted = ([torch.zeros_like(p, dtype=torch.bfloat16) for p in params] for _ in range(2))
+    a, b = optim.AdamW(params, bits=bits, copies=halves), optim.AdamW(other, bits=bits, copies=wanted)
+    old = [p.data for p in params] + [halves[1].data]
+    a.step(grads)
+    b.step(grads)
+    params[0].data, params[1].data, halves[1].data = params[0].clone(), params[1].clone(), halves[1].clone()
+    kept = [p.clone() for p in old]
+    a.step(grads)
+    b.step(grads)
+    assert all(torch.equal(p, q) for p, q in zip(params + halves, other + wanted))
+    assert all(torch.equal(p, q) for p, q in zip(old, kept))
+    for data in (torch.zeros(6, device="cuda"), torch.zeros(5, dtype=torch.float64, device="cuda"), params[1].data[:5],
+                 torch.zeros(10, device="cuda")[::2], torch.zeros(5)):
+        before = params[0].data
+        params[0].data = data
+        with pytest.raises(ValueError):
+            a.step(grads)
+        params[0].data = before
+    a.step(grads)
+    b.step(grads)
+    assert a.t == b.t == 3 and all(torch.equal(p, q) for p, q in zip(params + halves, other + wanted))
+
+
+def test_capture_without_device_step(cuda, optim):
+    """Replays would all be the step that was captured."""
+    torch = cuda
+    p, x = torch.ones(10, device="cuda"), torch.zeros((), device="cuda")
+    opt = optim.AdamW([p])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x.add_(1)
+        with pytest.raises(RuntimeError):
+            opt.step([p.clone()])
+    graph.replay()
+    torch.cuda.synchronize()
+    assert opt.t == 0 and (p == 1).all() and x == 1
+
+
 def test_elements_beyond_32_bits(cuda, optim):
     """One tensor of more than 2^32 elements: the last blocks, and those on either side of 2^32."""
     torch = cuda

@@ -208,6 +208,37 @@ def test_refusals(cuda, experts):
         experts.route(c, 1025)
 
 
+def test_results_apart_from_the_rows(cuda, experts):
+    """An out that shares elements with the arguments is refused; columns of one tensor beside one another are not."""
+    torch = cuda
+    T, k, d = 40, 1, 24
+    c = torch.arange(T, device="cuda", dtype=torch.int32).flip(0)[:, None].contiguous()
+    r = experts.route(c, T)
+    w = torch.full((T, k), 2.0, device="cuda")
+    wide = torch.randn(T, 3 * d + 1, device="cuda")
+    for dtype in (torch.float32, torch.bfloat16):
+        buf = wide.to(dtype)
+        x, y, z = buf[:, :d], buf[:, d:2 * d], buf[:, 2 * d:3 * d]
+        for call in (lambda: experts.spread(x, r, out=x), lambda: experts.spread(x, r, out=buf[:, d - 1:2 * d - 1]),
+                     lambda: experts.spread(y, r, out=buf[:, 1:d + 1]), lambda: experts.join(x, r, w, out=x),
+                     lambda: experts.join(x[:5], r, w, out=buf[:, d // 2:d // 2 + d]),
+                     lambda: experts.join_grad(x, y, r, w, out=x), lambda: experts.join_grad(x, y, r, w, out=buf[:, d + 1:2 * d + 1]),
+                     lambda: experts.spread(buf.view(-1)[:T * d].view(T, d), r, out=y), lambda: experts.join_grad(x, x, r, w, out=x)):
+            with pytest.raises(ValueError, match="share"):
+                call()
+        torch.cuda.synchronize()
+        assert torch.equal(buf, wide.to(dtype))
+        want = x.clone()
+        experts.spread(x, r, out=y)
+        assert torch.equal(y, want.flip(0)) and torch.equal(x, want)
+        experts.join(y, r, w, out=z)
+        assert torch.equal(z, 2 * want) and torch.equal(x, want)
+        dx = experts.join_grad(x, y, r, w, out=z)[0]
+        assert torch.equal(dx, 2 * want.flip(0)) and torch.equal(x, want) and torch.equal(y, want.flip(0))
+        one = experts.route(c[:1] * 0, 1)
+        assert torch.equal(experts.spread(x[3:4], one, out=x[4:5]), x[3:4])     # two rows of one tensor
+
+
 def test_streams_and_graphs(cuda, experts):
     torch = cuda
     T, k, E, d = 3000, 8, 64, 130
