@@ -512,14 +512,14 @@ __global__ void __launch_bounds__(kThreads, 3) adamw8_kernel(const __grid_consta
 
 // ---- host --------------------------------------------------------------------
 
-// CTAs of a launch: one for every 64 blocks, so that the SMs, which the memory does not serve alike, take them as
-// they come (75 M fp32 with 8-bit moments and copies: 183 us, 234 with equal shares for all CTAs that
-// fit at once); fewer blocks are spread over all that fit.
+// CTAs of a launch: as many as fit at once.  With 8-bit moments one for every 64 blocks, so that the SMs, which the
+// memory does not serve alike, take them as they come (100 M fp32 with copies: 243 us, 312 with equal shares for
+// all that fit); 32-bit moments want their shares in a row (403 M fp32: 1662 us, 1672 by 64 blocks; 72 M bf16: 249, 255).
 constexpr unsigned kBlocksOfCta = 64;
-unsigned grid_of(unsigned blocks, int each) {
+unsigned grid_of(unsigned blocks, int each, int bits) {
   int dev = 0, sms = 148;
   if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  return std::max(std::min((blocks + kWarps - 1) / kWarps, (unsigned)(sms * each)), blocks / kBlocksOfCta);
+  return std::max(std::min((blocks + kWarps - 1) / kWarps, (unsigned)(sms * each)), bits == 8 ? blocks / kBlocksOfCta : 0);
 }
 int ctas_of_an_sm(const void* kernel, int smem) {
   int each = 1;
@@ -537,7 +537,7 @@ cudaError_t launch(const Table& a, const Rates& r, int bits, cudaStream_t st) {
   static std::atomic<int> known[2];
   int each = known[bits == 8].load(std::memory_order_relaxed);
   if (!each) known[bits == 8].store(each = ctas_of_an_sm(reinterpret_cast<const void*>(kernel), smem), std::memory_order_relaxed);
-  kernel<<<grid_of(a.first[a.count], each), kThreads, smem, st>>>(a, r);
+  kernel<<<grid_of(a.first[a.count], each, bits), kThreads, smem, st>>>(a, r);
   return cudaGetLastError();
 }
 // The fast root takes a v below the smallest normal float, whose root is 1.1e-19, for 0: no

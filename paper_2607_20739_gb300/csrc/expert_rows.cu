@@ -278,7 +278,7 @@ struct Weights {
 
 // Pieces that a lane has in flight.
 template <int W>
-constexpr int spread_pieces() { return W == 16 ? 4 : 8; }
+constexpr int spread_pieces() { return W == 16 ? 2 : 4; }
 
 template <typename E, int W>
 __global__ void __launch_bounds__(kThreads) spread_kernel(Move a) {

@@ -23,6 +23,7 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kUnroll = 4;            // 16-byte pieces a thread has in flight
 constexpr int kMaxCluster = 8;
 constexpr int kMostTop = 64;
+constexpr int kFewTop = 16;
 
 struct Scores {
   const void* x;
@@ -168,6 +169,28 @@ __device__ __forceinline__ float warp_nth(float v, int n) {
       v = ((lane & o) == 0) == ((lane & size) == 0) ? fmaxf(v, other) : fminf(v, other);
     }
   return __shfl_sync(0xffffffffu, v, n - 1);
+}
+// What k of the warp's values reach, 32 times N of them: the largest such number of 16 bits, found bit by bit.
+// -infinity where fewer than k are above it.
+template <int N>
+__device__ __forceinline__ float warp_reached(const float (&v)[N], int k) {
+  uint32_t key[N], found = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t b = __float_as_uint(v[i]);
+    key[i] = b ^ ((int32_t)b < 0 ? 0xffffffffu : 0x80000000u);
+  }
+  for (uint32_t bit = 1u << 31; bit >= 1u << 16; bit >>= 1) {
+    const uint32_t next = found | bit;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) n += __popc(__ballot_sync(0xffffffffu, key[i] >= next));
+    if (n < k) continue;
+    found = next;
+    if (n == k) break;
+  }
+  if (found <= 0x007fffffu) return -INFINITY;                // the key of -infinity
+  return __uint_as_float(found ^ (found & 0x80000000u ? 0x80000000u : 0xffffffffu));
 }
 template <int G>
 __device__ __forceinline__ float least_bound(const Top<G>& sh) {
@@ -369,7 +392,9 @@ __device__ __forceinline__ Part scan(const E* x, const Slice& s, int tid, float 
   if (tid < s.head + (s.last - rest)) add_one(o, Elem<E>::get(x + (tid < s.head ? s.first + tid : rest + tid - s.head)), c);
   const uint4* p = reinterpret_cast<const uint4*>(x + body);
   const int groups = groups_of_part<G>(s);
-  float most = -INFINITY, halves[2] = {-INFINITY, -INFINITY};
+  float most = -INFINITY, each_most[kUnroll];
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) each_most[u] = -INFINITY;
   uint4 v[kUnroll];
   for (int i0 = 0, part = 0, left = groups; i0 < s.pieces; i0 += G * kUnroll) {
     const int i = i0 + tid;
@@ -378,9 +403,9 @@ __device__ __forceinline__ Part scan(const E* x, const Slice& s, int tid, float 
     add_pieces<E>(o, v, c);
     if (kMany) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint4 half[kUnroll / 2] = {v[h * kUnroll / 2], v[h * kUnroll / 2 + 1]};
-        halves[h] = fmaxf(halves[h], Elem<E>::top(half));
+      for (int u = 0; u < kUnroll; ++u) {
+        const uint4 one[1] = {v[u]};
+        each_most[u] = fmaxf(each_most[u], Elem<E>::top(one));
       }
     }
     if (!k || at_once<G>(s)) continue;
@@ -392,8 +417,7 @@ __device__ __forceinline__ Part scan(const E* x, const Slice& s, int tid, float 
     }
   }
   if (k) {
-    // a warp that has a whole row: k of its lanes, or half as many that have met it in both halves of their pieces
-    const float bound = kMany ? warp_nth(fminf(halves[0], halves[1]), (k + 1) / 2) : warp_nth(o.m, (k + G / 32 - 1) / (G / 32));
+    const float bound = kMany ? warp_reached(each_most, k) : warp_nth(o.m, (k + G / 32 - 1) / (G / 32));
     if (tid % 32 == 0) sh.warp_bound[tid / 32] = bound;
     if (tid == 0) sh.keys = sh.hots = 0;
     if (G == 32) __syncwarp();
@@ -923,7 +947,8 @@ int sm_count() {
 // Rows as in the losses' streaming passes: a warp takes one up to 4 KB, or 24 KB
 // where there are rows for all warps; few long rows are split over a cluster while the SMs hold more CTAs and a part
 // stays above 4 KB.
-constexpr int64_t kWarpRowBytes = 4 * 1024, kWarpManyRowsBytes = 24 * 1024, kWarpManyTopBytes = 72 * 1024;
+constexpr int64_t kWarpRowBytes = 4 * 1024, kWarpManyRowsBytes = 24 * 1024, kWarpFewTopBytes = 72 * 1024, kWarpTopBytes = 48 * 1024;
+constexpr int kWarpFewTop = 12;
 struct Shape {
   bool warp;
   int ranks;
@@ -931,7 +956,7 @@ struct Shape {
 };
 Shape shape_of(const pgc_logits* z, int k) {
   const int64_t bytes = z->classes * (z->dtype == PGC_BF16 ? 2 : 4), sms = sm_count();
-  const int64_t many = k ? kWarpManyTopBytes : kWarpManyRowsBytes;
+  const int64_t many = k == 0 ? kWarpManyRowsBytes : k <= kWarpFewTop ? kWarpFewTopBytes : kWarpTopBytes;
   Shape s{bytes <= kWarpRowBytes || (bytes <= many && z->rows >= 32 * sms), 1, 0};
   if (s.warp) {
     s.grid = (unsigned)((z->rows + kWarps - 1) / kWarps);
@@ -945,7 +970,10 @@ Shape shape_of(const pgc_logits* z, int k) {
 // Rows of bf16 whose elements can be taken in pairs, and rows that are held in registers: up to 128
 // classes by 8 lanes, 256 by 16, 512 by 32 (fp32, and bf16 in pairs).
 bool in_pairs(const pgc_logits* z) { return z->classes % 2 == 0 && z->ld % 2 == 0 && (uintptr_t)z->x % 4 == 0; }
-bool short_rows(const pgc_logits* z) { return z->classes <= (z->dtype == PGC_F32 || in_pairs(z) ? 512 : 256); }
+bool short_rows(const pgc_logits* z, int k) {
+  const bool wide = z->dtype == PGC_F32;
+  return z->classes <= (k ? (wide ? 256 : 512) : wide || in_pairs(z) ? 512 : 256);
+}
 unsigned short_grid(const pgc_logits* z) {
   const int64_t rows = kWarps * (z->classes <= 128 ? 4 : z->classes <= 256 ? 2 : 1);
   return (unsigned)((z->rows + rows - 1) / rows);
@@ -967,7 +995,7 @@ cudaError_t by_width(const pgc_logits* z, F f) {
   if (V <= 64) return two ? f.template operator()<H, 8, 8, 2>() : f.template operator()<H, 8, 8, 1>();
   if (V <= 128) return two ? f.template operator()<H, 8, 16, 2>() : f.template operator()<H, 8, 16, 1>();
   if (V <= 256) return two ? f.template operator()<H, 16, 16, 2>() : f.template operator()<H, 16, 16, 1>();
-  return f.template operator()<H, 32, 16, 2>();
+  return two ? f.template operator()<H, 32, 16, 2>() : f.template operator()<H, 32, 16, 1>();
 }
 struct ShortScores {
   const pgc_logits* z;
@@ -991,7 +1019,7 @@ struct ShortGrad {
 
 template <typename E>
 cudaError_t launch_scores(const Scores& a, const Shape& s, cudaStream_t st) {
-  const auto kernel = !s.warp ? scores_kernel<E, kThreads, false> : a.k > 32 ? scores_kernel<E, 32, true> : scores_kernel<E, 32, false>;
+  const auto kernel = !s.warp ? scores_kernel<E, kThreads, false> : a.k > kFewTop ? scores_kernel<E, 32, true> : scores_kernel<E, 32, false>;
   size_t smem = s.warp ? sizeof(Shared<32>) * kWarps : sizeof(Shared<kThreads>);
   if (s.ranks > 1) smem = (smem + 15) / 16 * 16 + sizeof(Gathered);
   cudaLaunchAttribute attr;
@@ -1041,7 +1069,7 @@ int pgc_token_scores(const pgc_logits *z, int32_t k, float *logp, float *entropy
   a.k = k; a.logp = logp; a.entropy = entropy; a.top = top; a.top_logp = top_logp;
   a.stats = reinterpret_cast<float2*>(stats);
   const cudaStream_t st = (cudaStream_t)stream;
-  if (short_rows(z)) return report_cuda(by_width(z, ShortScores{z, a, st}));
+  if (short_rows(z, k)) return report_cuda(by_width(z, ShortScores{z, a, st}));
   const Shape s = shape_of(z, k);
   return report_cuda(z->dtype == PGC_BF16 ? launch_scores<__nv_bfloat16>(a, s, st) : launch_scores<float>(a, s, st));
 }
@@ -1057,7 +1085,7 @@ int pgc_token_scores_grad(const pgc_logits *z, const float *stats, const float *
   a.stats = reinterpret_cast<float2*>(const_cast<float*>(stats));
   a.entropy = const_cast<float*>(entropy);
   const cudaStream_t st = (cudaStream_t)stream;
-  if (short_rows(z)) return report_cuda(by_width(z, ShortGrad{z, a, dlogp, dentropy, st}));
+  if (short_rows(z, 0)) return report_cuda(by_width(z, ShortGrad{z, a, dlogp, dentropy, st}));
   const Shape s = shape_of(z, 0);
   return report_cuda(z->dtype == PGC_BF16 ? launch_grad<__nv_bfloat16>(a, s, dlogp, dentropy, st)
                                           : launch_grad<float>(a, s, dlogp, dentropy, st));

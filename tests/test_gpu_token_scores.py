@@ -411,3 +411,31 @@ def test_short_rows(cuda, losses, dtype, V, k):
     assert torch.isnan(r["logp"][5:7]).all() and torch.isnan(r["entropy"][5:7]).all()
     assert r["top"][6, 0] == V // 2 and V // 2 not in r["top"][5].tolist()
     assert torch.isfinite(r["logp"][7:]).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("V", [258, 300, 520, 700, 1024, 1025, 2040])
+@pytest.mark.parametrize("k", [12, 13, 16, 17, 21, 48, 64])
+def test_bounds_of_a_warps_row(cuda, losses, dtype, V, k):
+    """Rows that a warp takes, where the parts that its lanes know the largest of are few, equal, empty or uneven."""
+    torch = cuda
+    dtype = getattr(torch, dtype)
+    g = torch.Generator(device="cuda").manual_seed(V * 100 + k)
+    x = torch.randn(14, V, generator=g, device="cuda") * 3
+    x[0] -= 100
+    for row, left in ((1, k - 1), (2, k), (3, k + 1)):
+        some = torch.randperm(V, generator=g, device="cuda")[left:]
+        x[row, some] = float("-inf")
+    x[4] = -2.5
+    x[5] = torch.arange(V, device="cuda") / 8
+    x[6] = -torch.arange(V, device="cuda") / 8
+    x[7] = torch.randn(V, generator=g, device="cuda") * 1e-38
+    x[8, :64] += 50                               # the largest side by side
+    x[9, ::32] += 50
+    x[10, ::256] += 50
+    x[11] = torch.where(torch.rand(V, generator=g, device="cuda") < 0.5, float(torch.finfo(dtype).min), -1e30)
+    x[11, torch.randperm(V, generator=g, device="cuda")[:k // 2]] = 1.0
+    x[12] = torch.where(torch.rand(V, generator=g, device="cuda") < 0.5, 0.0, -0.0)
+    x[13, :V // 2] = float("-inf")
+    x = x.to(dtype)
+    check_scores(torch, losses.token_scores(x, None, k), x, None, k, 1.0)
