@@ -147,6 +147,7 @@ __device__ __forceinline__ float value_of(Key q) {
 template <int G>
 struct Top {
   static constexpr int kKeys = G * 8 + kMostTop;            // the ones kept and a step of eight each
+  static constexpr int kFewKeys = G == 32 ? 160 : 2 * G;
   static constexpr int kParts = 8;
   Key key[kKeys];
   Key best[kMostTop];                                          // largest first, 0 where there is none
@@ -170,11 +171,11 @@ __device__ __forceinline__ float warp_nth(float v, int n) {
     }
   return __shfl_sync(0xffffffffu, v, n - 1);
 }
-// What k of the warp's values reach, 32 times N of them: the largest such number of 16 bits, found bit by bit.
-// -infinity where fewer than k are above it.
+// The least of the warp's values, 32 times N of them, that are at least the largest number of 16 bits, found bit by bit,
+// which k of them reach.  -infinity where fewer than k are above it.
 template <int N>
 __device__ __forceinline__ float warp_reached(const float (&v)[N], int k) {
-  uint32_t key[N], found = 0;
+  uint32_t key[N], found = 0, least = 0xffffffffu;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const uint32_t b = __float_as_uint(v[i]);
@@ -189,8 +190,10 @@ __device__ __forceinline__ float warp_reached(const float (&v)[N], int k) {
     found = next;
     if (n == k) break;
   }
-  if (found <= 0x007fffffu) return -INFINITY;                // the key of -infinity
-  return __uint_as_float(found ^ (found & 0x80000000u ? 0x80000000u : 0xffffffffu));
+#pragma unroll
+  for (int i = 0; i < N; ++i) least = min(least, key[i] >= found ? key[i] : least);
+  least = __reduce_min_sync(0xffffffffu, least);
+  return __uint_as_float(least ^ (least & 0x80000000u ? 0x80000000u : 0xffffffffu));
 }
 template <int G>
 __device__ __forceinline__ float least_bound(const Top<G>& sh) {
@@ -382,6 +385,91 @@ __device__ __forceinline__ void push_piece(const uint4& piece, int first, float 
 #pragma unroll
   for (int j = 0; j < Elem<E>::N; ++j) push(f[j], first + j, bound, sh);
 }
+// Where most parts reach the bound, by elements that are equal, as a rule: classes masked by a number, fewer than k
+// others left.  What lies above the bound is taken from the whole slice, and what is missing to k from the
+// lowest classes that have met it.
+template <typename E, int G>
+__device__ __noinline__ void top_of_ties(const E* x, Slice s, int tid, int k, float bound, Top<G>& sh) {
+  constexpr int N = Elem<E>::N;
+  const int body = s.first + s.head, rest = body + s.pieces * N;
+  const uint4* p = reinterpret_cast<const uint4*>(x + body);
+  sync_group<G>();
+  if (tid == 0) sh.keys = 0;
+  sync_group<G>();
+  auto put = [&](bool take, float f, int v) {
+    if (!take) return;
+    const int at = atomicAdd(&sh.keys, 1);
+    if (at < Top<G>::kKeys) sh.key[at] = key_of(f, (unsigned)v);
+  };
+  const int edge = tid < s.head ? s.first + tid : rest + tid - s.head;       // an element beside the pieces
+  const bool has_edge = tid < s.head + (s.last - rest);
+  const float at_edge = has_edge ? Elem<E>::get(x + edge) : -INFINITY;
+  put(at_edge > bound, at_edge, edge);
+  for (int i0 = tid; i0 < s.pieces; i0 += G * kUnroll) {
+    uint4 v[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) v[u] = i0 + u * G < s.pieces ? load16(p + i0 + u * G) : no_piece(Elem<E>::kLowest);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const uint4 one[1] = {v[u]};
+      if (!(Elem<E>::top(one) > bound)) continue;
+      float f[8];
+      each<E>(v[u], f);
+#pragma unroll
+      for (int j = 0; j < N; ++j) put(f[j] > bound, f[j], body + (i0 + u * G) * N + j);
+    }
+  }
+  sync_group<G>();
+  const int above = sh.keys;
+  int n = above;
+  if (n > Top<G>::kKeys) {
+    top_in_steps<E, G>(x, s, tid, k, sh);
+    return;
+  }
+  // elements of consecutive classes, thread after thread
+  auto append = [&](const float (&f)[8], int first) {
+    int mine = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) mine += f[j] == bound;
+    int up = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const int q = __shfl_up_sync(0xffffffffu, up, o);
+      if (tid % 32 >= o) up += q;
+    }
+    if (tid % 32 == 31) sh.red[tid / 32] = up;
+    sync_group<G>();
+    int at = n + up - mine;
+    for (int w = 0; w < G / 32; ++w) {
+      at += w < tid / 32 ? (int)sh.red[w] : 0;
+      n += (int)sh.red[w];
+    }
+    sync_group<G>();
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (f[j] == bound) {
+        if (at < k) sh.key[at] = key_of(f[j], (unsigned)(first + j));
+        ++at;
+      }
+  };
+  auto one = [&](bool has, float f, int v) {
+    float all[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) all[j] = j || !has ? NAN : f;
+    append(all, v);
+  };
+  sync_group<G>();
+  if (n < k) one(tid < s.head, at_edge, edge);
+  for (int i0 = 0; i0 < s.pieces && n < k; i0 += G) {
+    float f[8];
+    each<E>(i0 + tid < s.pieces ? load16(p + i0 + tid) : no_piece(Elem<E>::kLowest), f);
+    append(f, body + (i0 + tid) * N);
+  }
+  if (n < k) one(tid >= s.head && has_edge, at_edge, edge);
+  sync_group<G>();
+  rank_keys<G>(sh, sh.key, above < k ? min(n, k) : above, k, tid);
+}
+
 // A slice's sums in one pass, its parts' largest elements and the warps' bounds.
 // kMany: more alternatives than a warp has lanes.
 template <typename E, int G, bool kMany>
@@ -441,8 +529,8 @@ __device__ __forceinline__ void scan_top(const E* x, const Slice& s, int tid, in
     return;
   }
   const int body = s.first + s.head, rest = body + s.pieces * N, groups = groups_of_part<G>(s);
+  const int parts = s.pieces && !at_once<G>(s) ? ((s.pieces + G * kUnroll - 1) / (G * kUnroll) + groups - 1) / groups : 0;
   if (o.m >= bound) {
-    const int parts = s.pieces && !at_once<G>(s) ? ((s.pieces + G * kUnroll - 1) / (G * kUnroll) + groups - 1) / groups : 0;
     for (int q = 0; q < parts; ++q)
       if (sh.most[q * G + tid] >= bound) sh.hot[atomicAdd(&sh.hots, 1)] = (uint16_t)(q * G + tid);
     if (tid < s.head + (s.last - rest)) {
@@ -451,6 +539,10 @@ __device__ __forceinline__ void scan_top(const E* x, const Slice& s, int tid, in
     }
   }
   sync_group<G>();
+  if (sh.hots > max(parts * G / 2, 2 * k)) {
+    top_of_ties<E, G>(x, s, tid, k, bound, sh);
+    return;
+  }
   const unsigned per = groups * kUnroll, items = per * (unsigned)sh.hots;
   const uint4* p = reinterpret_cast<const uint4*>(x + body);
   for (unsigned i = tid; i < items; i += G * kUnroll) {
@@ -472,8 +564,8 @@ __device__ __forceinline__ void scan_top(const E* x, const Slice& s, int tid, in
   }
   sync_group<G>();
   const int n = sh.keys;
-  if (n <= Top<G>::kKeys) rank_keys<G>(sh, sh.key, n, k, tid);
-  else top_in_steps<E, G>(x, s, tid, k, sh);
+  if (n <= Top<G>::kFewKeys) rank_keys<G>(sh, sh.key, n, k, tid);
+  else top_of_ties<E, G>(x, s, tid, k, bound, sh);
 }
 
 // ---- a row -------------------------------------------------------------------------

@@ -439,3 +439,44 @@ def test_bounds_of_a_warps_row(cuda, losses, dtype, V, k):
     x[13, :V // 2] = float("-inf")
     x = x.to(dtype)
     check_scores(torch, losses.token_scores(x, None, k), x, None, k, 1.0)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("T,V,shift", [(12, 600, 1), (12, 1000, 3), (12, 2000, 0), (12, 2031, 5), (12, 9001, 1), (170, 9001, 3), (12, 40001, 7), (320, 40001, 2),
+                                       (5000, 6001, 1)])
+@pytest.mark.parametrize("k", [1, 5, 20, 64])
+def test_many_equal_ones_reach_the_bound(cuda, losses, dtype, T, V, shift, k):
+    """Fewer than k above the equal ones: they are the lowest classes among these, wherever they lie."""
+    torch = cuda
+    dtype = getattr(torch, dtype)
+    g = torch.Generator(device="cuda").manual_seed(V + k)
+    store = torch.empty(T * V + shift, dtype=dtype, device="cuda")
+    x = store[shift:].view(T, V)
+    lowest = float(torch.finfo(dtype).min)
+    values = torch.randn(12, V, generator=g, device="cuda").to(dtype)
+    perm = torch.randperm(V, generator=g, device="cuda")
+    for row, (left, mask) in enumerate([(k - 1, lowest), (k // 2, -1e9), (0, 0.0), (max(k - 2, 0), -3.0), (k, lowest), (k + 1, -1e30)]):
+        values[row, perm[left:]] = mask
+    values[6] = 0.0
+    values[6, V // 2:] = 1.0                      # nothing above, in the upper half
+    values[7] = -1.0
+    values[7, V // 3::2] = 4.0
+    values[7, perm[:k // 3]] = 5.0
+    values[8] = 2.0
+    values[8, :V - V // 4] = -values[8, :V - V // 4]
+    values[9] = (perm % 3).to(dtype)
+    values[10] = lowest
+    values[10, V - k // 2:] = 1.0                  # at the very end
+    values[11, perm[k // 2:]] = float("-inf")
+    x.copy_(values.repeat(-(-T // 12), 1)[:T])
+    some = torch.cat([torch.arange(12), torch.arange(T - 12, T)]).unique().cuda()
+    r = losses.token_scores(x, None, k)
+    if k < 2:                                     # the last row has no class left
+        none = some[some % 12 == 11]
+        assert r["entropy"][none].isnan().all() and (r["top"][none] == -1).all()
+        some = some[some % 12 != 11]
+    got = {name: v[some] for name, v in r.items() if v is not None}
+    got["logp"] = None
+    check_scores(torch, got, x[some], None, k, 1.0)
+    reps = r["top"][:T // 12 * 12].view(-1, 12, k)
+    assert (reps == reps[:1]).all()
