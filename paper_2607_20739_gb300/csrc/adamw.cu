@@ -211,6 +211,7 @@ __device__ __forceinline__ void store8(E* p, int lane, int64_t left, bool all, c
   }
 }
 
+// A block a warp at a time; memory bounds it (403 M fp32: 1657 us, 6.8 TB/s; 72 M bf16: 249).
 template <typename P, typename G, bool kExact>
 __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ Table a, const __grid_constant__ Rates r) {
   const Step s = step_of(r);
@@ -250,8 +251,8 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
 // 10 bytes an element (bf16 parameters and gradients) an SM has 55 issue slots for it while its share of memory moves, and
 // its unit of compares, shifts and logic half as many.  So shifts to the left are products, choices maxima, and a
 // second moment's values a table; what is rare (a value below the lowest code, a block without a scale) is put right
-// behind a branch.  About 58 instructions an element are left (82 as first written), and they are the bound: 75 M in 150 us, 5.1 TB/s.
-// With fp32 parameters memory is, 6.6 TB/s.
+// behind a branch.  About 58 instructions an element are left (82 as first written), and they are the bound: 72 M in 143 us, 5.0 TB/s.
+// With fp32 parameters memory is: 403 M with copies in 950 us, 6.8 TB/s.
 __device__ __forceinline__ Four decode_m(uint32_t codes) {
   uint32_t lo, hi;
   asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
@@ -324,7 +325,8 @@ struct Arrays {
 };
 // Blocks on their way: each warp copies its own next ones into a ring of places in shared memory (cp.async) and
 // waits for nobody else's.  Loads to registers of one block a warp are too few bytes in flight for the memory's
-// latency (72 M bf16: 242 us, 185 with three places, 154 with four, no more with six).
+// latency (100 M fp32 with bf16 gradients and copies: 243 us with four places, 257 with three, 244 with six; 72 M bf16,
+// which instructions bound, 143 with any, 242 through registers).
 constexpr int kPlaces = 4;
 template <typename P, typename G>
 struct Place {
@@ -512,14 +514,17 @@ __global__ void __launch_bounds__(kThreads, 3) adamw8_kernel(const __grid_consta
 
 // ---- host --------------------------------------------------------------------
 
-// CTAs of a launch: as many as fit at once.  With 8-bit moments one for every 64 blocks, so that the SMs, which the
-// memory does not serve alike, take them as they come (100 M fp32 with copies: 243 us, 312 with equal shares for
-// all that fit); 32-bit moments want their shares in a row (403 M fp32: 1662 us, 1672 by 64 blocks; 72 M bf16: 249, 255).
-constexpr unsigned kBlocksOfCta = 64;
-unsigned grid_of(unsigned blocks, int each, int bits) {
+// CTAs of a launch: as many as fit at once, or more of `per` blocks each, which the SMs take as they come: the memory does not serve
+// all alike, and 8-bit moments with fp32 parameters are bound by it (100 M with copies: 243 us with 64 blocks each, 312 with
+// equal shares for all that fit; 75 M: 184, 191 with 128).  bf16 parameters, bound by instructions, lose less to the CTAs'
+// first loads with 128 (72 M in 55 tensors: 151 us, 155 with 64).  32-bit moments want their shares in a row
+// (403 M fp32: 1662 us, 1672 by 64 blocks; 72 M bf16: 249, 255).
+template <typename P>
+unsigned blocks_of_cta(int bits) { return bits == 32 ? 0 : sizeof(P) == 2 ? 128 : 64; }
+unsigned grid_of(unsigned blocks, int each, unsigned per) {
   int dev = 0, sms = 148;
   if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  return std::max(std::min((blocks + kWarps - 1) / kWarps, (unsigned)(sms * each)), bits == 8 ? blocks / kBlocksOfCta : 0);
+  return std::max(std::min((blocks + kWarps - 1) / kWarps, (unsigned)(sms * each)), per ? blocks / per : 0);
 }
 int ctas_of_an_sm(const void* kernel, int smem) {
   int each = 1;
@@ -537,7 +542,7 @@ cudaError_t launch(const Table& a, const Rates& r, int bits, cudaStream_t st) {
   static std::atomic<int> known[2];
   int each = known[bits == 8].load(std::memory_order_relaxed);
   if (!each) known[bits == 8].store(each = ctas_of_an_sm(reinterpret_cast<const void*>(kernel), smem), std::memory_order_relaxed);
-  kernel<<<grid_of(a.first[a.count], each, bits), kThreads, smem, st>>>(a, r);
+  kernel<<<grid_of(a.first[a.count], each, blocks_of_cta<P>(bits)), kThreads, smem, st>>>(a, r);
   return cudaGetLastError();
 }
 // The fast root takes a v below the smallest normal float, whose root is 1.1e-19, for 0: no

@@ -184,8 +184,9 @@ __global__ void __launch_bounds__(kRouteThreads) place_kernel(Route a) {
 // rows start between two words.  (16-byte pieces put together from the two that hold them were slower: 90
 // instructions a piece, 109 us where 4-byte pieces take 55: join of 10000 x 6 x 1001 fp32.)  What is left
 // behind the last piece is taken by single elements.  All three kernels are bound by memory:
-// at 16 bytes they move 6.1 to 6.6 TB/s (bf16, 16384 x 8 x 2048: spread 96 us, join 96, gradient 174), at 4 bytes
-// fp32 5.1 to 5.8, at 2 bytes 3.2 to 5.0.
+// at 16 bytes they move 6.1 to 6.6 TB/s (bf16, 16384 x 8 x 2048: spread 95 us, join 95, gradient 174), at 4 bytes
+// fp32 5.1 to 5.8, at 2 bytes 3.2 to 5.0.  16 bytes and 4, bf16: join 8192 x 4 x 5120 67 and 78 us, gradient
+// 174 and 199, spread 95 both.
 
 struct Move {
   const void* x;                // spread: tokens; join, join_grad: the experts' rows
@@ -276,7 +277,8 @@ struct Weights {
   __device__ __forceinline__ float operator[](int j) const { return __shfl_sync(0xffffffffu, j < 32 ? lo : hi, j & 31); }
 };
 
-// Pieces that a lane has in flight.
+// Pieces that a lane has in flight: two or four (10000 x 6 x 1001 fp32: 47 us, 52 with half as many; 16384 x 8 x 2048 bf16: 94.5 us,
+// 96.5 with twice as many, and few tokens make more warps: 8 x 8 x 2048 2.3 us on the GPU, 3.3).
 template <int W>
 constexpr int spread_pieces() { return W == 16 ? 2 : 4; }
 
@@ -308,7 +310,7 @@ __global__ void __launch_bounds__(kThreads) spread_kernel(Move a) {
   }
 }
 
-constexpr int kJoinRows = 4;          // rows that a lane has in flight, with U pieces of each
+constexpr int kJoinRows = 4;          // rows that a lane has in flight, with U pieces of each (8192 x 4 x 5120: 67 us; two 77, eight 163)
 template <int W>
 constexpr int join_pieces() { return W == 16 ? 2 : 8; }
 
@@ -486,8 +488,8 @@ int sm_count() {
   return n;
 }
 
-// CTAs of a sort: one does up to 2048 slots (2.7 us for 64 on the GPU, 12.7 for 8000, which three kernels take 6 for); above,
-// each has 1024 at least.  65536 x 8 of 256: 14.8 us, 34.2 where every CTA read all counts itself.
+// CTAs of a sort: one does up to 2048 slots (2.6 us for 64 on the GPU; 5.3 for 2048, three kernels 6.3; 14.8 for 8000, three kernels 6.3);
+// above, each has 1024 at least.  65536 x 8 of 256: 14.8 us, 34.2 where every CTA read all counts itself.
 constexpr int kAloneSlots = 2048;
 int route_ctas(int64_t n) {
   return n <= kAloneSlots ? 1 : (int)std::min<int64_t>((n + 1023) / 1024, kMostRouteCtas);
@@ -499,7 +501,8 @@ int width_of(std::initializer_list<uintptr_t> starts) {
   for (const uintptr_t p : starts) all |= p;
   return all % 16 == 0 ? 16 : all % 4 == 0 ? 4 : 2;
 }
-// A token is a warp's where there are tokens for the SMs' warps, else a CTA's.
+// A token is a warp's where there are tokens for the SMs' warps, else a CTA's: join 8192 x 4 x 5120 67 us by warps, 74 by CTAs, 65536 x 2 x
+// 1024 70 and 208; 1000 x 8 x 2048 13 and 9, its gradient 16 and 13.
 bool by_warps(const Move& a) { return a.T >= sm_count() * 32; }
 unsigned grid_of(const Move& a, bool warps) { return (unsigned)(warps ? (a.T + kWarps - 1) / kWarps : a.T); }
 

@@ -7,6 +7,12 @@
 //   logp = q_y,   H = -sum_v p_v q_v = L - sum_v e_v z_v / sum_v e_v,  z = (x - m) / tau, e = exp z,
 //   d logp / d x_v = ([v = y] - p_v) / tau,   d H / d x_v = -p_v (q_v + H) / tau.
 // Every term of H is positive, so nothing cancels.
+//
+// Long rows are bound by memory: one pass makes the sums and finds a bound that the k likeliest classes reach, and
+// only the few parts of a row that reach it are read again (4096 x 131072 bf16, k = 20: 189 us, 5.7 TB/s; the pass
+// alone 165, without alternatives 158; pushing what may be among the k while the pass runs took 255 to 277).  Short
+// rows are bound by their own instructions, few rows by latencies.  The gradient is one pass (2000 x 50001 fp32: 115 us,
+// 7.0 TB/s read and written).
 #include <algorithm>
 #include <cmath>
 
@@ -23,6 +29,8 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kUnroll = 4;            // 16-byte pieces a thread has in flight
 constexpr int kMaxCluster = 8;
 constexpr int kMostTop = 64;
+// Up to as many alternatives of a warp's row come from a bound that sorts the lanes' maxima; more from one that counts those of four
+// parts a lane: 65536 x 2000 bf16, k = 16: 114 us, 125 by counts; 20000 x 32768, k = 20: 304, 336 by sorting; k = 32: 344, 614.
 constexpr int kFewTop = 16;
 
 struct Scores {
@@ -62,7 +70,7 @@ __device__ __forceinline__ void add_one(Part& o, float f, float c) {
   o.w += times_log(e, z);
 }
 // A piece with -inf as -2^100 (NaN stays NaN), so that 2^z z is 0 there and not NaN: one instruction for
-// two bf16.  An element below -2^100 adds nothing in a row that is not `extreme` (kSmallC).
+// two bf16.  An element below -2^100 adds nothing but with a c below 2^-70, where such a row is summed apart (part_extreme).
 template <typename E>
 __device__ __forceinline__ uint4 above(uint4 v);
 template <>
@@ -128,11 +136,12 @@ __device__ __forceinline__ void sync_group() {
 }
 
 // ---- the k largest ---------------------------------------------------------------
-// Every lane knows the largest of its elements, and of up to eight parts of them.  The r-th largest
-// of a warp's 32, with r = k over the group's warps, is reached by r elements of this warp, the least of the warps'
-// such bounds by k of the row: only what reaches it can be among the k largest.  The parts that do, a few more
-// than k, are read again (from the L2 cache, as a rule), and what reaches the bound there is ranked.  Keys order
-// by value and then by the lower class; no two are equal.
+// Every lane knows the largest of its elements, and of up to eight parts of them (4096 x 131072 bf16, k = 20: 195 us
+// where four parts took 204 and sixteen 214).  The r-th largest of a warp's 32, with r = k over the group's warps, is reached by
+// r elements of this warp, the least of the warps' such bounds by k of the row: only what reaches it can be among
+// the k largest.  (A bound from the ranks of all 256 maxima is tighter and slower: 241 us.)  The parts that do, a few more than k,
+// are read again (from the L2 cache, as a rule), and what reaches the bound there is ranked.  Keys order by value and
+// then by the lower class; no two are equal.  Finding parts, reading and ranking them take 12, 10 and 8 us of the 195.
 
 __device__ __forceinline__ Key key_of(float f, unsigned v) {
   const uint32_t b = __float_as_uint(f + 0.f);              // zeros of both signs are equal
@@ -147,7 +156,7 @@ __device__ __forceinline__ float value_of(Key q) {
 template <int G>
 struct Top {
   static constexpr int kKeys = G * 8 + kMostTop;            // the ones kept and a step of eight each
-  static constexpr int kFewKeys = G == 32 ? 160 : 2 * G;
+  static constexpr int kFewKeys = G == 32 ? 160 : 2 * G;     // more are equal ones, as a rule
   static constexpr int kParts = 8;
   Key key[kKeys];
   Key best[kMostTop];                                          // largest first, 0 where there is none
@@ -258,9 +267,8 @@ __device__ __forceinline__ void each(const uint4& v, float (&f)[8]) {
 #pragma unroll
   for (int i = 0; i < Elem<E>::N / 2; ++i) split(h[i], f[2 * i], f[2 * i + 1]);
 }
-// A slice's pieces in steps of one a thread, keeping the k largest so far: for rows
-// where more elements reach the bound than there are places, mostly classes that are
-// masked by a number, fewer than k others left.
+// A slice's pieces in steps of one a thread, keeping the k largest so far: for rows where more different elements
+// reach the bound than there are places (rising ones: 4096 x 131072 bf16, k = 64: 640 us, other rows 213).
 template <typename E, int G>
 __device__ __noinline__ void top_in_steps(const E* x, Slice s, int tid, int k, Top<G>& sh) {
   constexpr int N = Elem<E>::N;
@@ -387,7 +395,7 @@ __device__ __forceinline__ void push_piece(const uint4& piece, int first, float 
 }
 // Where most parts reach the bound, by elements that are equal, as a rule: classes masked by a number, fewer than k
 // others left.  What lies above the bound is taken from the whole slice, and what is missing to k from the
-// lowest classes that have met it.
+// lowest classes that have met it (4096 x 131072 bf16, 10 classes left, k = 20: 308 us, 1205 in steps; others 189).
 template <typename E, int G>
 __device__ __noinline__ void top_of_ties(const E* x, Slice s, int tid, int k, float bound, Top<G>& sh) {
   constexpr int N = Elem<E>::N;
@@ -668,7 +676,8 @@ __device__ __forceinline__ void write_none(const Scores& a, int64_t t, int tid) 
   a.stats[t] = make_float2(0.f, 0.f);
 }
 
-// A row per warp (G = 32), CTA or cluster of CTAs.
+// A row per warp (G = 32), CTA or cluster of CTAs.  Five CTAs an SM (16384 x 32768 bf16, k = 5: 192 us; 197 with four, 266 with six);
+// warps in fp32 four (20000 x 8192, k = 20: 157, 186 with five).
 template <typename E, int G, bool kMany>
 __global__ void __launch_bounds__(kThreads, G == 32 && sizeof(E) == 4 ? 4 : 5) scores_kernel(Scores a) {
   extern __shared__ __align__(16) unsigned char raw[];
@@ -733,7 +742,7 @@ __global__ void __launch_bounds__(kThreads, G == 32 && sizeof(E) == 4 ? 4 : 5) s
 
 // ---- short rows --------------------------------------------------------------------
 // Rows of up to L R classes in the registers of L lanes, so that a warp has 32 / L rows at once:
-// what a row costs there is its own instructions, not its bytes.  Elements are single ones, or (P = 2: bf16
+// what a row costs there is its own instructions, not its bytes (131072 x 100 bf16: 20 us, 46 with k = 20; in pieces 66 and 393).  Elements are single ones, or (P = 2: bf16
 // rows of even length and pitch that start on 4 bytes) two neighbours.
 template <int L, int P>
 __device__ __forceinline__ int short_at(int l, int j) { return P * (l + j / P * L) + j % P; }
@@ -1036,9 +1045,12 @@ int sm_count() {
   return n;
 }
 
-// Rows as in the losses' streaming passes: a warp takes one up to 4 KB, or 24 KB
-// where there are rows for all warps; few long rows are split over a cluster while the SMs hold more CTAs and a part
-// stays above 4 KB.
+// A warp takes a row of up to 4 KB; where there are rows for all warps, up to 24 KB (36621 x 8192 bf16: 101 us, 163 by CTAs; the
+// gradient's 183, 206; up to 72 KB no gain: 16384 x 32768 bf16 171 and 173, gradient 313 and 336), and with alternatives, whose
+// barriers a CTA waits at, up to 72 KB (20000 x 32768, k = 5: 239 us, 284 by CTAs; fp32 of 8192, k = 20: 149, 209) or, above
+// 12 of them, 48 KB (20000 x 24000, k = 32: 261, 284; 32768, k = 32: 349, 318).  Few long rows are split over a
+// cluster while the SMs hold more CTAs and a part stays above 4 KB (one row of 131072, k = 20: 9.0 us on the
+// GPU, 13.1 by one CTA).
 constexpr int64_t kWarpRowBytes = 4 * 1024, kWarpManyRowsBytes = 24 * 1024, kWarpFewTopBytes = 72 * 1024, kWarpTopBytes = 48 * 1024;
 constexpr int kWarpFewTop = 12;
 struct Shape {
@@ -1060,7 +1072,9 @@ Shape shape_of(const pgc_logits* z, int k) {
 }
 
 // Rows of bf16 whose elements can be taken in pairs, and rows that are held in registers: up to 128
-// classes by 8 lanes, 256 by 16, 512 by 32 (fp32, and bf16 in pairs).
+// classes by 8 lanes, 256 by 16, 512 by 32.  Their limit, with both sides in us for 65536 rows (registers, then pieces):
+// 512 bf16, k = 5: 58, 64; k = 20: 91, 89; k = 64: 184, 879; 301 bf16, one by one, k = 20: 91, 97; 256 fp32, k = 5: 56, 57; k = 20: 85, 80;
+// k = 64: 165, 569; 512 fp32, whose keys have 64 bits, k = 5: 109, 60; k = 64: 347, 160.  Without alternatives as in the losses.
 bool in_pairs(const pgc_logits* z) { return z->classes % 2 == 0 && z->ld % 2 == 0 && (uintptr_t)z->x % 4 == 0; }
 bool short_rows(const pgc_logits* z, int k) {
   const bool wide = z->dtype == PGC_F32;
@@ -1128,7 +1142,8 @@ cudaError_t launch_scores(const Scores& a, const Shape& s, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
-// The gradient takes a longer row in parts of 32 KB at least, few rows in as many as a cluster would have CTAs.
+// The gradient takes a longer row in parts of 32 KB at least, few rows in as many as a cluster would have CTAs: 2000 x 50001 fp32
+// 122 us, 132 in whole rows, 136 in parts of 16 KB; 4096 x 131072 bf16 310, 323, 357.
 constexpr int64_t kGradPartBytes = 32 * 1024;
 template <typename E>
 cudaError_t launch_grad(const Scores& a, const Shape& s, const float* dlogp, const float* dentropy, cudaStream_t st) {

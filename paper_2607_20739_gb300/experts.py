@@ -83,12 +83,9 @@ def _share(a, b):
     start_a, start_b = a.data_ptr(), b.data_ptr()
     if start_a + ((rows_a - 1) * ld_a + d) * size <= start_b or start_b + ((rows_b - 1) * ld_b + d) * size <= start_a:
         return False
-    if rows_a < 2 or rows_b < 2:
-        pitch = max(a.stride(0), b.stride(0))
-    elif ld_a == ld_b:
-        pitch = ld_a
-    else:
+    if rows_a < 2 and rows_b < 2 or rows_a > 1 and rows_b > 1 and ld_a != ld_b:
         return True
+    pitch = ld_a if rows_a > 1 else ld_b
     # columns beside one another in rows of a common pitch
     apart = (start_b - start_a) % (pitch * size)
     return not d * size <= apart <= (pitch - d) * size

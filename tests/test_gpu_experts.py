@@ -237,6 +237,12 @@ def test_results_apart_from_the_rows(cuda, experts):
         assert torch.equal(dx, 2 * want.flip(0)) and torch.equal(x, want) and torch.equal(y, want.flip(0))
         one = experts.route(c[:1] * 0, 1)
         assert torch.equal(experts.spread(x[3:4], one, out=x[4:5]), x[3:4])     # two rows of one tensor
+        with pytest.raises(ValueError, match="share"):
+            experts.spread(x[3:4], one, out=buf[3:4, d - 1:2 * d - 1])
+        few = experts.route(c[:1] * 0, 1)
+        assert torch.equal(experts.spread(x[3:4], few, out=z[2:6])[:1], x[3:4])   # a row and columns beside it
+        with pytest.raises(ValueError, match="share"):
+            experts.spread(x[3:4], few, out=buf[2:6, 1:d + 1])
 
 
 def test_streams_and_graphs(cuda, experts):
