@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
 // 10 bytes an element (bf16 parameters and gradients) an SM has 55 issue slots for it while its share of memory moves, and
 // its unit of compares, shifts and logic half as many.  So shifts to the left are products, choices maxima, and a
 // second moment's values a table; what is rare (a value below the lowest code, a block without a scale) is put right
-// behind a branch.  About 58 instructions an element are left (82 as first written), and they are the bound: 72 M in 143 us, 5.0 TB/s.
+// behind a branch.  About 58 instructions an element are left (82 as first written), and they are the bound: 72 M in 133 us, 5.4 TB/s.
 // With fp32 parameters memory is: 403 M with copies in 950 us, 6.8 TB/s.
 __device__ __forceinline__ Four decode_m(uint32_t codes) {
   uint32_t lo, hi;
@@ -325,8 +325,8 @@ struct Arrays {
 };
 // Blocks on their way: each warp copies its own next ones into a ring of places in shared memory (cp.async) and
 // waits for nobody else's.  Loads to registers of one block a warp are too few bytes in flight for the memory's
-// latency (100 M fp32 with bf16 gradients and copies: 243 us with four places, 257 with three, 244 with six; 72 M bf16,
-// which instructions bound, 143 with any, 242 through registers).
+// latency (72 M bf16: 242 us as first written, 185 with three places, 154 with four).  Now 100 M fp32 with bf16 gradients and copies
+// take 242 us with four, 256 with three, 242 with six; with fp32 gradients 244, and 324 with six, whose memory leaves room for two CTAs.
 constexpr int kPlaces = 4;
 template <typename P, typename G>
 struct Place {
@@ -425,8 +425,11 @@ __device__ __forceinline__ void step8(Pair (&p)[kPairs], const Pair (&g)[kPairs]
   }
 }
 
+// bf16 parameters: as many registers as it likes (124, two CTAs an SM), for the instructions bound it: 72 M in 55
+// tensors 139 us, 143 with the registers of two CTAs asked for, 150 of three.  fp32 parameters: three CTAs (100 M with
+// copies 242 us, 247 with two).
 template <typename P, typename G, bool kExact>
-__global__ void __launch_bounds__(kThreads, 3) adamw8_kernel(const __grid_constant__ Table a, const __grid_constant__ Rates r) {
+__global__ void __launch_bounds__(kThreads, sizeof(P) == 2 ? 1 : 3) adamw8_kernel(const __grid_constant__ Table a, const __grid_constant__ Rates r) {
   using Q = Place<P, G>;
   extern __shared__ __align__(16) unsigned char ring[];
   __shared__ float values[256];
@@ -517,7 +520,7 @@ __global__ void __launch_bounds__(kThreads, 3) adamw8_kernel(const __grid_consta
 // CTAs of a launch: as many as fit at once, or more of `per` blocks each, which the SMs take as they come: the memory does not serve
 // all alike, and 8-bit moments with fp32 parameters are bound by it (100 M with copies: 243 us with 64 blocks each, 312 with
 // equal shares for all that fit; 75 M: 184, 191 with 128).  bf16 parameters, bound by instructions, lose less to the CTAs'
-// first loads with 128 (72 M in 55 tensors: 151 us, 155 with 64).  32-bit moments want their shares in a row
+// first loads with 128 (72 M in 55 tensors: 139 us, 143 with 96).  32-bit moments want their shares in a row
 // (403 M fp32: 1662 us, 1672 by 64 blocks; 72 M bf16: 249, 255).
 template <typename P>
 unsigned blocks_of_cta(int bits) { return bits == 32 ? 0 : sizeof(P) == 2 ? 128 : 64; }
