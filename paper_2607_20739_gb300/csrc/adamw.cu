@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
 // 10 bytes an element (bf16 parameters and gradients) an SM has 55 issue slots for it while its share of memory moves, and
 // its unit of compares, shifts and logic half as many.  So shifts to the left are products, choices maxima, and a
 // second moment's values a table; what is rare (a value below the lowest code, a block without a scale) is put right
-// behind a branch.  About 58 instructions an element are left (82 as first written), and they are the bound: 72 M in 133 us, 5.4 TB/s.
+// behind a branch.  About 53 instructions an element are left (82 as first written), and they are the bound: 72 M in 133 us, 5.4 TB/s.
 // With fp32 parameters memory is: 403 M with copies in 950 us, 6.8 TB/s.
 __device__ __forceinline__ Four decode_m(uint32_t codes) {
   uint32_t lo, hi;
