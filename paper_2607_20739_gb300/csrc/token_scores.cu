@@ -393,6 +393,53 @@ __device__ __forceinline__ void push_piece(const uint4& piece, int first, float 
 #pragma unroll
   for (int j = 0; j < Elem<E>::N; ++j) push(f[j], first + j, bound, sh);
 }
+// Which of the elements of kUnroll pieces reach the bound, a bit each, and where a bit's element is.  (A bf16 pair is
+// compared at once; the bound is a bf16 number there.)
+template <typename E>
+struct Reach;
+template <>
+struct Reach<float> {
+  __device__ __forceinline__ static uint32_t bits(const uint4 (&v)[kUnroll], float bound) {
+    uint32_t r = 0;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) r |= __uint_as_float(w[j]) >= bound ? 1u << (4 * u + j) : 0u;
+    }
+    return r;
+  }
+  __device__ __forceinline__ static int piece(int bit) { return bit / 4; }
+  __device__ __forceinline__ static int element(int bit) { return bit % 4; }
+};
+template <>
+struct Reach<__nv_bfloat16> {
+  __device__ __forceinline__ static uint32_t bits(const uint4 (&v)[kUnroll], float bound) {
+    const __nv_bfloat162 b = __float2bfloat162_rn(bound);
+    uint32_t r = 0;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) r |= __hge2_mask(*reinterpret_cast<const __nv_bfloat162*>(&w[j]), b) & 0x00010001u << (4 * u + j);
+    }
+    return r;
+  }
+  __device__ __forceinline__ static int piece(int bit) { return bit % 16 / 4; }
+  __device__ __forceinline__ static int element(int bit) { return bit % 4 * 2 + bit / 16; }
+};
+// Those elements' keys, read again one by one, as they are few; first(u): the class that piece u starts with.
+template <typename E, int G, typename F>
+__device__ __forceinline__ void push_pieces(const E* x, const uint4 (&v)[kUnroll], float bound, Top<G>& sh, F first) {
+  uint32_t bits = Reach<E>::bits(v, bound);
+  if (!bits) return;
+  int at = atomicAdd(&sh.keys, __popc(bits));
+  for (; bits && at < Top<G>::kKeys; bits &= bits - 1, ++at) {
+    const int bit = __ffs(bits) - 1, c = first(Reach<E>::piece(bit)) + Reach<E>::element(bit);
+    sh.key[at] = key_of(Elem<E>::get(x + c), (unsigned)c);
+  }
+}
+
 // Where most parts reach the bound, by elements that are equal, as a rule: classes masked by a number, fewer than k
 // others left.  What lies above the bound is taken from the whole slice, and what is missing to k from the
 // lowest classes that have met it (4096 x 131072 bf16, 10 classes left, k = 20: 308 us, 1205 in steps; others 189).
@@ -518,11 +565,7 @@ __device__ __forceinline__ Part scan(const E* x, const Slice& s, int tid, float 
     if (tid == 0) sh.keys = sh.hots = 0;
     if (G == 32) __syncwarp();
     if (at_once<G>(s) && bound > -INFINITY) {
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const uint4 one[1] = {v[u]};
-        if (tid + u * G < s.pieces && Elem<E>::top(one) >= bound) push_piece<E, G>(v[u], body + (tid + u * G) * N, bound, sh);
-      }
+      push_pieces<E, G>(x, v, bound, sh, [&](int u) { return body + (tid + u * G) * N; });
     }
   }
   return o;
