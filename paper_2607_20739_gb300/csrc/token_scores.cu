@@ -1116,12 +1116,14 @@ Shape shape_of(const pgc_logits* z, int k) {
 
 // Rows of bf16 whose elements can be taken in pairs, and rows that are held in registers: up to 128
 // classes by 8 lanes, 256 by 16, 512 by 32.  Their limit, with both sides in us for 65536 rows (registers, then pieces):
-// 512 bf16, k = 5: 58, 64; k = 20: 91, 89; k = 64: 184, 879; 301 bf16, one by one, k = 20: 91, 97; 256 fp32, k = 5: 56, 57; k = 20: 85, 80;
-// k = 64: 165, 569; 512 fp32, whose keys have 64 bits, k = 5: 109, 60; k = 64: 347, 160.  Without alternatives as in the losses.
+// 512 bf16, k = 5: 58, 60; k = 12: 74, 65; k = 20: 91, 85; k = 64: 183, 717; 301 bf16, one by one, k = 12: 72, 69; k = 20: 89, 95;
+// 256 bf16, k = 12: 38, 64; 256 fp32, k = 5: 56, 56; k = 12: 70, 62; k = 20: 85, 81; k = 64: 165, 441; 130 fp32, k = 12: 68, 66; k = 20: 83, 87;
+// 100 fp32, k = 12: 36, 56; 512 fp32, whose keys have 64 bits, k = 5: 109, 60; k = 64: 347, 160.  Without alternatives as in the losses.
 bool in_pairs(const pgc_logits* z) { return z->classes % 2 == 0 && z->ld % 2 == 0 && (uintptr_t)z->x % 4 == 0; }
 bool short_rows(const pgc_logits* z, int k) {
   const bool wide = z->dtype == PGC_F32;
-  return z->classes <= (k ? (wide ? 256 : 512) : wide || in_pairs(z) ? 512 : 256);
+  if (!k) return z->classes <= (wide || in_pairs(z) ? 512 : 256);
+  return z->classes <= (wide ? 256 : 512) / (k > 8 && k <= kFewTop ? 2 : 1);
 }
 unsigned short_grid(const pgc_logits* z) {
   const int64_t rows = kWarps * (z->classes <= 128 ? 4 : z->classes <= 256 ? 2 : 1);
