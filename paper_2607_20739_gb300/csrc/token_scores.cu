@@ -30,7 +30,7 @@ constexpr int kUnroll = 4;            // 16-byte pieces a thread has in flight
 constexpr int kMaxCluster = 8;
 constexpr int kMostTop = 64;
 // Up to as many alternatives of a warp's row come from a bound that sorts the lanes' maxima; more from one that counts those of four
-// parts a lane: 65536 x 2000 bf16, k = 16: 114 us, 125 by counts; 20000 x 32768, k = 20: 304, 336 by sorting; k = 32: 344, 614.
+// parts a lane: 65536 x 2000 bf16, k = 16: 113 us, 125 by counts; 1000, k = 20: 87, 83 by sorting; k = 32: 105, 325; 20000 x 8192 fp32: 173, 305.
 constexpr int kFewTop = 16;
 
 struct Scores {
@@ -719,8 +719,8 @@ __device__ __forceinline__ void write_none(const Scores& a, int64_t t, int tid) 
   a.stats[t] = make_float2(0.f, 0.f);
 }
 
-// A row per warp (G = 32), CTA or cluster of CTAs.  Five CTAs an SM (16384 x 32768 bf16, k = 5: 192 us; 197 with four, 266 with six);
-// warps in fp32 four (20000 x 8192, k = 20: 157, 186 with five).
+// A row per warp (G = 32), CTA or cluster of CTAs.  Five CTAs an SM (16384 x 32768 bf16, k = 5: 194 us; 198 with four, 267 with six);
+// warps in fp32 four (20000 x 8192, k = 20: 148, 160 with five).
 template <typename E, int G, bool kMany>
 __global__ void __launch_bounds__(kThreads, G == 32 && sizeof(E) == 4 ? 4 : 5) scores_kernel(Scores a) {
   extern __shared__ __align__(16) unsigned char raw[];
