@@ -310,16 +310,18 @@ __global__ void __launch_bounds__(kThreads) spread_kernel(Move a) {
   }
 }
 
-constexpr int kJoinRows = 4;          // rows that a lane has in flight, with U pieces of each (8192 x 4 x 5120: 67 us; two 77, eight 163)
-template <int W>
-constexpr int join_pieces() { return W == 16 ? 2 : 8; }
+// Rows that a lane has in flight (Q: four, or two where k is no more), and pieces of each: 8192 x 4 x 5120 bf16 67 us, 77 with two
+// rows, 163 with eight; 30000 x 2 x 2048 60 us, 63 with four rows of two pieces; 30000 x 2 x 1001 fp32 57, 62 with four of eight;
+// 30000 x 2 x 2002 bf16, whose sums are two a piece, 59, with 16 pieces 142.
+template <typename E, int W, int Q>
+constexpr int join_pieces() { return W == 16 ? (Q == 2 ? 3 : 2) : Q == 4 ? 8 : W > (int)sizeof(E) ? 12 : 16; }
 
 // A token per warp (G = 32) or CTA, in a loop over its row: a warp for each part of a row
 // spent its time on the places and weights (8192 x 4 x 5120 bf16: 98 us, 58 this way).
-template <typename E, int W, int G>
+template <typename E, int W, int Q, int G>
 __global__ void __launch_bounds__(kThreads, 4) join_kernel(Move a) {
   using A = Access<E, W>;
-  constexpr int N = A::N, U = join_pieces<W>(), Q = kJoinRows;
+  constexpr int N = A::N, U = join_pieces<E, W, Q>();
   const int tid = threadIdx.x % G;
   const int64_t t = G == 32 ? blockIdx.x * (int64_t)kWarps + threadIdx.x / 32 : blockIdx.x;
   if (t >= a.T) return;
@@ -375,16 +377,18 @@ __global__ void __launch_bounds__(kThreads, 4) join_kernel(Move a) {
   }
 }
 
-template <int W>
-constexpr int grad_pieces() { return W == 16 ? 1 : 3; }
+// Pieces of a row that a lane has in flight, with Q rows: as many as registers allow.  30000 x 2 x 2048 bf16 94 us, 101 with one
+// of 16 bytes; 15000 x 4 x 1001 fp32 88, 98 with three of 4; 10000 x 6 x 1001 90, 93 with three, 97 with eight; 8000 x 8 x 1001 104, 109 with four.
+template <int W, int Q>
+constexpr int grad_pieces() { return W == 16 ? (Q <= 4 ? 2 : 1) : Q == 8 ? 3 : Q == 6 ? 5 : 8; }
 
 // A token per warp or CTA: the products with its own row are summed over all of it.  Q rows at
-// once: the least of 2, 4 and 8 that takes k, or 8 (65536 x 2 x 1024 bf16: 108 us, 137 with 8), for which three CTAs an
-// SM matter more than registers (16384 x 8 x 2048 bf16: 174 us, 226 with two).  In place too: a lane reads what it writes before it does.
+// once: the least of 2, 4, 6 and 8 that takes k, or 8 (65536 x 2 x 1024 bf16: 101 us, 137 with 8), for which three CTAs an
+// SM matter more than registers (16384 x 8 x 2048 bf16: 175 us, 226 with two).  In place too: a lane reads what it writes before it does.
 template <typename E, int W, int Q, int G>
 __global__ void __launch_bounds__(kThreads, Q == 2 ? 4 : 3) join_grad_kernel(Move a) {
   using A = Access<E, W>;
-  constexpr int N = A::N, U = grad_pieces<W>();
+  constexpr int N = A::N, U = grad_pieces<W, Q>();
   __shared__ float red[kWarps][kMaxChoices];
   const int lane = threadIdx.x % 32, tid = threadIdx.x % G, warp = threadIdx.x / 32;
   const int64_t t = G == 32 ? blockIdx.x * (int64_t)kWarps + warp : blockIdx.x;
@@ -513,15 +517,17 @@ cudaError_t launch_spread(Move a, cudaStream_t st) {
   spread_kernel<E, W><<<(unsigned)((a.T * a.chunks + kWarps - 1) / kWarps), kThreads, 0, st>>>(a);
   return cudaGetLastError();
 }
+template <typename E, int W, int G>
+auto join_of(int k) { return k <= 2 ? join_kernel<E, W, 2, G> : join_kernel<E, W, 4, G>; }
 template <typename E, int W>
 cudaError_t launch_join(const Move& a, cudaStream_t st) {
   const bool warps = by_warps(a);
-  (warps ? join_kernel<E, W, 32> : join_kernel<E, W, kThreads>)<<<grid_of(a, warps), kThreads, 0, st>>>(a);
+  (warps ? join_of<E, W, 32>(a.k) : join_of<E, W, kThreads>(a.k))<<<grid_of(a, warps), kThreads, 0, st>>>(a);
   return cudaGetLastError();
 }
 template <typename E, int W, int G>
 auto join_grad_of(int k) {
-  return k <= 2 ? join_grad_kernel<E, W, 2, G> : k <= 4 ? join_grad_kernel<E, W, 4, G> : join_grad_kernel<E, W, 8, G>;
+  return k <= 2 ? join_grad_kernel<E, W, 2, G> : k <= 4 ? join_grad_kernel<E, W, 4, G> : k <= 6 ? join_grad_kernel<E, W, 6, G> : join_grad_kernel<E, W, 8, G>;
 }
 template <typename E, int W>
 cudaError_t launch_join_grad(const Move& a, cudaStream_t st) {

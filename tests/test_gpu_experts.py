@@ -342,3 +342,32 @@ def test_moves_of_many_tokens(cuda, experts, dtype, k, d, pad, shift):
     terms = e.double()[at] * dy.double()[:, None, :] * on[:, :, None]
     chain = min(d, d / 32 + 64) + 1
     assert ((dweight.double() - terms.sum(2)).abs() <= U * chain * terms.abs().sum(2)).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("T,k,d", [(5000, 1, 2002), (5000, 2, 1030), (5100, 2, 769), (300, 2, 5001), (40, 1, 9000), (5000, 3, 1031), (5000, 5, 650),
+                                   (5000, 6, 331), (200, 6, 4098), (5000, 7, 100)])
+def test_moves_of_each_number_of_rows(cuda, experts, dtype, T, k, d):
+    """The kernels' numbers of rows at once, with rows that are longer than a step of theirs and end inside one."""
+    torch = cuda
+    dtype = getattr(torch, dtype)
+    r = routes_of(torch, experts, place_of(torch, T, k, T * k, seed=d))
+    e, dy = rows(torch, dtype, T * k, d, seed=1), rows(torch, dtype, T, d, seed=2)
+    w = torch.rand(T, k, device="cuda") + 0.5
+    y = experts.join(e, r, w)
+    de, dw = experts.join_grad(dy, e, r, w, out=torch.zeros_like(e))
+    # on the host, where an index out of range is an error
+    e, dy, w, y, de, dw, place = (t.double().cpu() if t.is_floating_point() else t.long().cpu() for t in (e, dy, w, y, de, dw, r.place))
+    on = (place >= 0) & (place < T * k)
+    taken = e[torch.where(on, place, 0)] * on[..., None]                         # [T, k, d]
+    want = (taken * w[..., None]).sum(1)
+    size = (taken.abs() * w[..., None]).sum(1)
+    half = torch.finfo(dtype).eps / 2
+    # k roundings of products and sums, then that of the result
+    assert ((y - want).abs() <= (k + 1) * 2.0 ** -24 * size + half * want.abs() * (1 + 1e-6) + 1e-38).all()
+    prod = taken * dy[:, None]
+    # every sum of d terms in one order or another
+    assert ((dw - prod.sum(2)).abs() <= (d + 2) * 2.0 ** -24 * prod.abs().sum(2) + 1e-38).all()
+    want = torch.zeros_like(e)
+    want[place[on]] = (w[..., None] * dy[:, None])[on]
+    assert ((de - want).abs() <= (2.0 ** -24 + half) * want.abs() * (1 + 1e-6) + 1e-38).all()
