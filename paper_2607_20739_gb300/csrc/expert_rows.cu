@@ -310,8 +310,8 @@ __global__ void __launch_bounds__(kThreads) spread_kernel(Move a) {
   }
 }
 
-// Rows that a lane has in flight (Q: four, or two where k is no more), and pieces of each: 8192 x 4 x 5120 bf16 67 us, 77 with two
-// rows, 163 with eight; 30000 x 2 x 2048 60 us, 63 with four rows of two pieces; 30000 x 2 x 1001 fp32 57, 62 with four of eight;
+// Rows that a lane has in flight (Q: four, or two where k is no more), and pieces of each: 16384 x 8 x 2048 bf16 95 us, 99 with two
+// rows, 158 with eight; 30000 x 2 x 2048 60 us, 63 with four rows of two pieces; 30000 x 2 x 1001 fp32 57, 62 with four of eight;
 // 30000 x 2 x 2002 bf16, whose sums are two a piece, 59, with 16 pieces 142.
 template <typename E, int W, int Q>
 constexpr int join_pieces() { return W == 16 ? (Q == 2 ? 3 : 2) : Q == 4 ? 8 : W > (int)sizeof(E) ? 12 : 16; }
