@@ -85,7 +85,8 @@ class AdamW:
         t = 0 if state is None else int(state["t"])
         if t < 0:
             raise ValueError("the number of steps must not be negative")
-        self._device_step = torch.full((), t, dtype=torch.int64, device=self.device) if device_step and self.params else None
+        # the number of the next step: raised behind a step that was taken
+        self._next = torch.full((), t + 1, dtype=torch.int64, device=self.device) if device_step and self.params else None
         self._t = t
         self._table = (B.AdamWTensor * len(self.params))()
         # the column of the gradients' addresses
@@ -194,7 +195,7 @@ class AdamW:
     @property
     def t(self) -> int:
         """Steps made (read from the device, and waited for, with device_step)."""
-        return int(self._device_step.item()) if self._device_step is not None else self._t
+        return int(self._next.item()) - 1 if self._next is not None else self._t
 
     def state(self):
         """What ``state`` takes: the step and the moments (the tensors themselves)."""
@@ -245,17 +246,17 @@ class AdamW:
         self._grads[:] = addresses
 
         def call(st):
-            if self._device_step is not None:
-                self._device_step.add_(1)
-            elif torch.cuda.is_current_stream_capturing():
+            if self._next is None and torch.cuda.is_current_stream_capturing():
                 raise RuntimeError("a step that is captured needs device_step: replays would all be the same step")
             a = B.AdamW(0.0 if lr_at is not None else self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay,
-                        self._t + 1, _address(self._device_step), _address(lr_at), _address(grad_scale),
+                        self._t + 1, _address(self._next), _address(lr_at), _address(grad_scale),
                         self.seed & 0xffffffff, _TYPES[self.params[0].dtype], _TYPES[dtype], self.bits)
             B._check(B.lib.pgc_adamw_step(a, self._table, len(self._table), st), "pgc_adamw_step")
+            if self._next is not None:
+                self._next.add_(1)
         kept = ()
         if stream is not None:
-            kept = [*self.params, *self._moments, *(self.copies or []), *grads, lr_at, grad_scale, self._device_step]
+            kept = [*self.params, *self._moments, *(self.copies or []), *grads, lr_at, grad_scale, self._next]
         _on(device, stream, kept, call)
         self._t += 1
         torch.autograd.graph.increment_version(self._versioned)

@@ -17,7 +17,7 @@ def array(address, n, kind=C.c_float):
 def optim(libpgc, monkeypatch):
     """optim.AdamW on the host; the calls that were made in optim.calls, as (step, sizes)."""
     from paper_2607_20739_gb300 import optim
-    calls, made = [], []
+    calls, made, library = [], [], libpgc.lib.pgc_adamw_step
     begin = optim.AdamW.__init__
 
     def watched(self, *args, **kw):
@@ -33,8 +33,9 @@ def optim(libpgc, monkeypatch):
                 yield (*(x.data_ptr() for x in t), t[0].numel())
 
     def step(s, table, count, stream):
-        if not np.isfinite([s.lr, s.eps, s.weight_decay]).all() or not 0 <= s.beta1 < 1 or not 0 <= s.beta2 < 1:
-            return libpgc.EINVAL
+        code = library(s, table, 0, stream)                      # what it says of the rates
+        if code:
+            return code
         t = array(s.step_at, 1, C.c_int64)[0] if s.step_at else s.step
         lr = array(s.lr_at, 1)[0] if s.lr_at else s.lr
         for e in table:
@@ -199,3 +200,27 @@ def test_the_number_of_parameters_stays(optim):
     with pytest.raises(ValueError, match="3 parameters"):
         a.step(grads[:1])
     assert a.t == 1
+
+
+@pytest.mark.parametrize("device_step", [False, True])
+def test_a_refused_step_does_not_count(optim, device_step):
+    """Whoever refuses it: the library the rates, the checks of tensors the rest."""
+    from paper_2607_20739_gb300 import PGCError
+    params, other, a, b, grads = pair(optim, device_step=device_step, betas=(0.9, 0.99))
+    a.step(grads)
+    b.step(grads)
+    before = [p.clone() for p in params]
+    for name, bad in (("lr", float("nan")), ("eps", -1.0), ("betas", (0.9, 1.0)), ("weight_decay", float("inf"))):
+        good = getattr(a, name)
+        setattr(a, name, bad)
+        with pytest.raises(PGCError):
+            a.step(grads)
+        setattr(a, name, good)
+    for bad in (grads[:2], [grads[0].double(), *grads[1:]], [None, grads[0], grads[2]]):
+        with pytest.raises(ValueError):
+            a.step(bad)
+    assert a.t == a.state()["t"] == 1 and same(params, before)
+    for _ in range(2):
+        a.step(grads)
+        b.step(grads)
+    assert a.t == b.t == 3 and same(params, other) and [t for t, _ in optim.calls] == [1, 1, 2, 2, 3, 3]

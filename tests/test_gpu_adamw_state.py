@@ -87,3 +87,35 @@ def test_moments_on_the_host_are_refused(cuda, optim, bits):
     a.step(grads)
     b.step(grads)
     assert same(torch, params, other) and a.t == 2
+
+
+@pytest.mark.parametrize("device_step", [False, True])
+def test_a_refused_step_does_not_count(cuda, optim, device_step):
+    """Nor does it leave anything else behind: captured and replayed steps go on as if it had not been."""
+    torch = cuda
+    from paper_2607_20739_gb300 import PGCError
+    params, other, a, b, grads = pair(torch, optim, 8, device_step=device_step)
+    a.step(grads)
+    b.step(grads)
+    a.lr = float("nan")
+    with pytest.raises(PGCError):
+        a.step(grads)
+    a.lr, a.eps = b.lr, -1.0
+    with pytest.raises(PGCError):
+        a.step(grads)
+    a.eps = b.eps
+    assert a.t == 1
+    if device_step:
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            a.step(grads)
+        graph.replay()
+        graph.replay()
+    else:
+        a.step(grads)
+        a.step(grads)
+    b.step(grads)
+    b.step(grads)
+    assert a.t == b.t == 3
+    assert same(torch, params, other) and same(torch, moments(a), moments(b))
