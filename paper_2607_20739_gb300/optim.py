@@ -85,8 +85,11 @@ class AdamW:
         t = 0 if state is None else int(state["t"])
         if t < 0:
             raise ValueError("the number of steps must not be negative")
-        # the number of the next step: raised behind a step that was taken
-        self._next = torch.full((), t + 1, dtype=torch.int64, device=self.device) if device_step and self.params else None
+        self._next = None
+        if device_step and self.params:
+            with torch.inference_mode(False):
+                # the number of the next step: raised behind a step that was taken
+                self._next = torch.full((), t + 1, dtype=torch.int64, device=self.device)
         self._t = t
         self._table = (B.AdamWTensor * len(self.params))()
         # the column of the gradients' addresses
@@ -164,7 +167,8 @@ class AdamW:
                 ("v_scale", torch.float32, blocks))
 
     def _zeros(self):
-        return tuple(torch.zeros(shape(p), dtype=dtype, device=p.device) for _, dtype, shape in self._formats() for p in self.params)
+        with torch.inference_mode(False):
+            return tuple(torch.zeros(shape(p), dtype=dtype, device=p.device) for _, dtype, shape in self._formats() for p in self.params)
 
     def _given_moments(self, groups):
         return tuple(t for name, dtype, shape in self._formats() for t in _list(name, groups[name], self.params, dtype, shape))

@@ -224,3 +224,20 @@ def test_a_refused_step_does_not_count(optim, device_step):
         a.step(grads)
         b.step(grads)
     assert a.t == b.t == 3 and same(params, other) and [t for t, _ in optim.calls] == [1, 1, 2, 2, 3, 3]
+
+
+def test_made_in_inference_mode(optim):
+    """What the optimizer makes for itself may be changed outside of it."""
+    params, grads = tensors(*SHAPES), tensors(*SHAPES, seed=1)
+    other = [p.clone() for p in params]
+    with torch.inference_mode():
+        a = optim.AdamW(params, device_step=True)
+        a.step(grads)
+    b = optim.AdamW(other)
+    b.step(grads)
+    for t, u in zip(a.m + a.v, b.m + b.v):
+        t.mul_(0.5)
+        u.mul_(0.5)
+    a.step(grads)
+    b.step(grads)
+    assert a.t == 2 and same(params, other)
