@@ -36,7 +36,7 @@ def optim(libpgc, monkeypatch):
         code = library(s, table, 0, stream)                      # what it says of the rates
         if code:
             return code
-        t = array(s.step_at, 1, C.c_int64)[0] if s.step_at else s.step
+        t = int(array(s.step_at, 1, C.c_int64)[0]) if s.step_at else s.step
         lr = array(s.lr_at, 1)[0] if s.lr_at else s.lr
         for e in table:
             if not e.grad or not e.n:
