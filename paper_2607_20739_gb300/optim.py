@@ -78,7 +78,7 @@ class AdamW:
             raise ValueError("bits must be 8 or 32")
         self._check_params()
         self.device = self.params[0].device if self.params else None
-        self.lr, self.betas, self.eps, self.weight_decay, self.bits, self.seed = lr, betas, eps, weight_decay, bits, seed
+        self.lr, self.betas, self.eps, self.weight_decay, self._bits, self.seed = lr, betas, eps, weight_decay, bits, seed
         self.copies = None if copies is None else _list("copies", copies, self.params, torch.bfloat16)
         self._moments = self._zeros() if state is None else self._given_moments(state)
         self._which = () if state is None else None         # who gave the moments may have them
@@ -176,6 +176,11 @@ class AdamW:
     def _groups(self):
         n = len(self._table)
         return {name: list(self._moments[i * n:(i + 1) * n]) for i, (name, _, _) in enumerate(self._formats())}
+
+    @property
+    def bits(self) -> int:
+        """Of the moments."""
+        return self._bits
 
     @property
     def m(self):

@@ -241,3 +241,16 @@ def test_made_in_inference_mode(optim):
     a.step(grads)
     b.step(grads)
     assert a.t == 2 and same(params, other)
+
+
+def test_bits_stay(optim):
+    """Those of the moments that were made: a step would read them as others'."""
+    params, other, a, b, grads = pair(optim)
+    with pytest.raises(AttributeError):
+        a.bits = 8
+    with pytest.raises(AttributeError):
+        a.m = b.m
+    assert a.bits == 32
+    a.step(grads)
+    b.step(grads)
+    assert same(params, other)
