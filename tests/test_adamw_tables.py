@@ -13,10 +13,13 @@ def array(address, n, kind=C.c_float):
     return np.ctypeslib.as_array((kind * n).from_address(address))
 
 
-@pytest.fixture
-def optim(libpgc, monkeypatch):
-    """optim.AdamW on the host; the calls that were made in optim.calls, as (step, sizes)."""
+@pytest.fixture(params=["torch's check", "lists"])
+def optim(libpgc, monkeypatch, request):
+    """optim.AdamW on the host; the calls that were made in optim.calls, as (step, sizes).  Also where torch
+    has no check of layouts in one call."""
     from paper_2607_20739_gb300 import optim
+    if request.param == "lists":
+        monkeypatch.setattr(optim, "_guard", lambda tensors: lambda *_: False)
     calls, made, library = [], [], libpgc.lib.pgc_adamw_step
     begin = optim.AdamW.__init__
 
@@ -254,3 +257,32 @@ def test_bits_stay(optim):
     a.step(grads)
     b.step(grads)
     assert same(params, other)
+
+
+def test_gradients_of_another_layout(optim):
+    """Gradients may change their type, objects and places between steps, not their shapes or strides."""
+    params, other, a, b, grads = pair(optim)
+    for _ in range(3):
+        a.step(grads)
+        b.step([g.clone() for g in grads])
+    for bad in (grads[0].t(), grads[0][:3], grads[0].view(-1), grads[0].double(), grads[0].bfloat16(), torch.zeros(5, 10)[:, ::2], 3.0):
+        with pytest.raises((ValueError, TypeError)):
+            a.step([bad, *grads[1:]])
+        data, good = grads[0].data, isinstance(bad, torch.Tensor)
+        if good:
+            grads[0].data = bad
+            with pytest.raises(ValueError):
+                a.step(grads)
+            grads[0].data = data
+    for p in params + grads:
+        p.requires_grad_(True)
+    with torch.no_grad():
+        a.step(grads)
+    b.step([g.detach() for g in grads])
+    for g in (grads, [None, *grads[1:]], grads):
+        a.step(g)
+        b.step(g)
+    twice = [grads[0], grads[1], grads[0][:4, :].reshape(-1)[:1].expand(4, 7).contiguous()]
+    a.step(twice)
+    b.step(twice)
+    assert a.t == b.t and same(params, other) and same(a.m + a.v, b.m + b.v)
