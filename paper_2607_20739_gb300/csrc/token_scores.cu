@@ -11,8 +11,8 @@
 // Long rows are bound by memory: one pass makes the sums and finds a bound that the k likeliest classes reach, and
 // only the few parts of a row that reach it are read again (4096 x 131072 bf16, k = 20: 189 us, 5.7 TB/s; the pass
 // alone 165, without alternatives 158; pushing what may be among the k while the pass runs took 255 to 277).  Short
-// rows are bound by their own instructions, few rows by latencies.  The gradient is one pass (2000 x 50001 fp32: 115 us,
-// 7.0 TB/s read and written).
+// rows are bound by their own instructions, few rows by latencies.  The gradient is one pass (2000 x 50001 fp32: 122 us,
+// 6.5 TB/s read and written; 115 where a row in eight has no target and is only written).
 #include <algorithm>
 #include <cmath>
 
@@ -136,12 +136,13 @@ __device__ __forceinline__ void sync_group() {
 }
 
 // ---- the k largest ---------------------------------------------------------------
-// Every lane knows the largest of its elements, and of up to eight parts of them (4096 x 131072 bf16, k = 20: 195 us
-// where four parts took 204 and sixteen 214).  The r-th largest of a warp's 32, with r = k over the group's warps, is reached by
+// Every lane knows the largest of its elements, and of up to eight parts of them (4096 x 131072 bf16, k = 20: 190 us,
+// 199 with four parts and 207 with sixteen).  The r-th largest of a warp's 32, with r = k over the group's warps, is reached by
 // r elements of this warp, the least of the warps' such bounds by k of the row: only what reaches it can be among
 // the k largest.  (A bound from the ranks of all 256 maxima is tighter and slower: 241 us.)  The parts that do, a few more than k,
 // are read again (from the L2 cache, as a rule), and what reaches the bound there is ranked.  Keys order by value and
-// then by the lower class; no two are equal.  Finding parts, reading and ranking them take 12, 10 and 8 us of the 195.
+// then by the lower class; no two are equal.  Finding parts, reading and ranking them took 12, 10 and 8 us
+// when the whole took 195.
 
 __device__ __forceinline__ Key key_of(float f, unsigned v) {
   const uint32_t b = __float_as_uint(f + 0.f);              // zeros of both signs are equal
@@ -590,6 +591,9 @@ __device__ __forceinline__ void scan_top(const E* x, const Slice& s, int tid, in
     }
   }
   sync_group<G>();
+  // (A warp's row of one part or two never has so many for k from 32 on, one in registers for any k: equal elements show there
+  // only when their keys are too many.  65536 x 2000 bf16, k = 40: 176 us, 603 with 10 classes left and the others at the lowest number;
+  // 600, k = 20: 84, 174.)
   if (sh.hots > max(parts * G / 2, 2 * k)) {
     top_of_ties<E, G>(x, s, tid, k, bound, sh);
     return;
@@ -785,7 +789,9 @@ __global__ void __launch_bounds__(kThreads, G == 32 && sizeof(E) == 4 ? 4 : 5) s
 
 // ---- short rows --------------------------------------------------------------------
 // Rows of up to L R classes in the registers of L lanes, so that a warp has 32 / L rows at once:
-// what a row costs there is its own instructions, not its bytes (131072 x 100 bf16: 20 us, 46 with k = 20; in pieces 66 and 393).  Elements are single ones, or (P = 2: bf16
+// what a row costs there is its own instructions and one load's latency, not its bytes (131072 x 100 bf16, which are 3.9 us of
+// memory: 12.0 us from a graph, 28 with k = 5, 43 with k = 20, 2.6 to 3.1 instructions a cycle and SM of 4; by calls, which the host
+// makes in 20 us, in pieces 66 and, with k = 20, 393).  Elements are single ones, or (P = 2: bf16
 // rows of even length and pitch that start on 4 bytes) two neighbours.
 template <int L, int P>
 __device__ __forceinline__ int short_at(int l, int j) { return P * (l + j / P * L) + j % P; }
@@ -1027,6 +1033,8 @@ __global__ void __launch_bounds__(kThreads) scores_grad_kernel(Scores a, int par
   if (target >= 0 && at >= 0 && at < s.pieces * N && at / N % G == tid) Elem<E>::put(g + target, slope_at(xy, true, r));
 }
 
+// Short rows: 131072 x 100 bf16 18.6 us from a graph (memory 7.8; the log probability's alone 14.2), 65536 x 512 39 (20; 27): 2.5 to 2.7
+// instructions a cycle and SM of 4, compares and selects of every element's extreme case and target among them.
 template <typename E, int L, int R, int P>
 __global__ void __launch_bounds__(kThreads) short_scores_grad_kernel(Scores a, const float* dlogp, const float* dentropy) {
   const int lane = threadIdx.x % 32, l = lane % L;
@@ -1093,7 +1101,8 @@ int sm_count() {
 // barriers a CTA waits at, up to 72 KB (20000 x 32768, k = 5: 239 us, 284 by CTAs; fp32 of 8192, k = 20: 149, 209) or, above
 // 12 of them, 48 KB (20000 x 24000, k = 32: 261, 284; 32768, k = 32: 349, 318).  Few long rows are split over a
 // cluster while the SMs hold more CTAs and a part stays above 4 KB (one row of 131072, k = 20: 9.0 us on the
-// GPU, 13.1 by one CTA).
+// GPU, 13.1 by one CTA).  Where these bounds cost: 8192 x 32768 fp32, k = 5: 193 us by CTAs, 183 by warps; 64 x 32768, k = 20: 8.4 us by clusters, 7.9
+// by CTAs.
 constexpr int64_t kWarpRowBytes = 4 * 1024, kWarpManyRowsBytes = 24 * 1024, kWarpFewTopBytes = 72 * 1024, kWarpTopBytes = 48 * 1024;
 constexpr int kWarpFewTop = 12;
 struct Shape {
