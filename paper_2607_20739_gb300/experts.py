@@ -51,6 +51,8 @@ def route(choice, experts, *, stream=None):
     tokens, k = choice.shape
     device = choice.device
     _vector("choice", choice, torch.int32, (tokens, k), device)
+    if not 1 <= experts <= 1024:            # before it is cut to 32 bits
+        raise B.PGCError(B.EINVAL if experts < 1 else B.ENOTSUP, "pgc_route")
     size = _bytes("pgc_route_workspace", tokens, k, experts)
 
     def call(st):

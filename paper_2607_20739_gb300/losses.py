@@ -86,14 +86,16 @@ def token_scores(logits, target=None, k=0, temperature=1.0, *, stream=None):
     """
     rows, classes, ld = _matrix("logits", logits)
     device = logits.device
+    if not 0 <= k <= 64:                    # before outputs are made for them
+        raise B.PGCError(B.EINVAL if k < 0 else B.ENOTSUP, "pgc_token_scores")
     if target is not None:
         _vector("target", target, torch.int32, (rows,), device)
 
     def call(st):
         logp = None if target is None else torch.empty(rows, dtype=torch.float32, device=device)
         entropy = torch.empty(rows, dtype=torch.float32, device=device)
-        top = torch.empty((rows, max(k, 0)), dtype=torch.int32, device=device)
-        top_logp = torch.empty((rows, max(k, 0)), dtype=torch.float32, device=device)
+        top = torch.empty((rows, k), dtype=torch.int32, device=device)
+        top_logp = torch.empty((rows, k), dtype=torch.float32, device=device)
         stats = torch.empty((rows, 2), dtype=torch.float32, device=device)
         z = B.Logits(logits.data_ptr(), _address(target), None, rows, classes, ld, 0, _TYPES[logits.dtype], temperature)
         B._check(B.lib.pgc_token_scores(z, k, _address(logp), entropy.data_ptr(), top.data_ptr(), top_logp.data_ptr(),

@@ -106,7 +106,7 @@ class AdamW:
                   themselves are used); default: zeros
     device_step   the number of steps is kept on the device, so that a captured step
                   counts itself when it is replayed; without it a step under capture is refused.  Rates that
-                  are floats are those of the capture in every replay
+                  are floats, and the places of all tensors, are those of the capture in every replay
 
     All parameters decay alike; those that should not (norms, biases) are another optimizer's, with a seed of its own.
     Data of parameters, copies and moments may be exchanged between steps (``t.data = ...``, off the GPU and back
